@@ -1,12 +1,15 @@
 """Compile the HIP library for gfx950 in-tree (hipcc cross-compiles without a GPU)."""
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libvmsreplay.so")
 SOURCES = ["vms_replay.hip", "vms_demo.hip", "vms_live.hip", "vms_peaks.hip"]
-HEADERS = ["wave_hw.hpp", "wave_ops.hpp", "replay_plan.hpp", "replay_kernels.hpp", "replay_fine.hpp", "selftest.hpp", "../../include/vms_replay.h", "../../include/vms_live.h"]
+OPS_SOURCES = ["vms_dropout.hip", "vms_norm.hip", "vms_lowrank.hip"]
+HEADERS = ["ops_common.hpp", "../../include/vms_ops.h", "wave_hw.hpp", "wave_ops.hpp", "replay_plan.hpp", "replay_kernels.hpp", "replay_fine.hpp", "selftest.hpp", "../../include/vms_replay.h", "../../include/vms_live.h"]
 
 # The replay loops branch on wave-uniform conditions only (whatever would switch lanes off is written
 # with selects or kept in non-inlined functions).  With the option below LLVM leaves such regions as
@@ -24,12 +27,16 @@ HIPCC_FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-shared", "-fPIC",
                "-Xclang", "-disable-lifetime-markers",
                "-Wno-inline-asm"]       # write_lane() names m0, which the compiler reserves but does not use here
 
+# The operators' kernels are loops over wide tensors: the compiler's own scheduling, for many wavefronts a SIMD.
+OPS_FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-shared", "-fPIC", "-Wall",
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+
 
 def _stale():
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS]
+    deps = [os.path.join(CSRC, s) for s in SOURCES + OPS_SOURCES + HEADERS]
     return any(os.path.exists(d) and os.path.getmtime(d) > t for d in deps)
 
 
@@ -37,17 +44,28 @@ def build(force=False, save_temps_dir=None):
     """Build libvmsreplay.so next to this file; returns its path."""
     if not force and not _stale():
         return LIB
-    srcs = [os.path.join(CSRC, s) for s in SOURCES if os.path.exists(os.path.join(CSRC, s))]
-    cmd = ["hipcc"] + HIPCC_FLAGS + ["-o", LIB] + srcs
-    cwd = CSRC
+    jobs = [(s, flags) for group, flags in ((SOURCES, HIPCC_FLAGS), (OPS_SOURCES, OPS_FLAGS)) for s in group]
     if save_temps_dir:
         os.makedirs(save_temps_dir, exist_ok=True)
-        cmd.append("--save-temps")
-        cwd = save_temps_dir
+    with tempfile.TemporaryDirectory() as objects:
+        def compile_one(job):
+            source, flags = job
+            obj = os.path.join(objects, source + ".o")
+            cmd = ["hipcc"] + [f for f in flags if f != "-shared"] + ["-c", os.path.join(CSRC, source), "-o", obj]
+            return obj, _run(cmd + ["--save-temps"] * bool(save_temps_dir), save_temps_dir or CSRC)
+        with ThreadPoolExecutor(4) as pool:
+            done = list(pool.map(compile_one, jobs))
+        out = "\n".join(text for _, text in done if text.strip())
+        _run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + [obj for obj, _ in done], CSRC)
+    if out:
+        print(out)
+    return LIB
+
+
+def _run(cmd, cwd):
+    """The command's own words; raises where it fails."""
     r = subprocess.run(cmd, cwd=cwd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     out = "\n".join(l for l in r.stdout.splitlines() if "packed-fp32-ops" not in l)
     if r.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + out)
-    if out.strip():
-        print(out)
-    return LIB
+    return out

@@ -1,0 +1,585 @@
+// vms_layernorm and vms_layernorm_backward (include/vms_ops.h).
+//
+// Both passes are bound by memory: a row is read once, kept in registers (group g of eight columns in
+// lane g mod LANES of those that share the row) and written once.  Mean and variance are taken in one
+// go without the cancellation of a difference of squares: every wavefront takes the mean of its part
+// and the squares around that, and the parts are joined by
+//     M2 = sum M2_w + sum n_w (mean_w - mean)^2.
+#include "ops_common.hpp"
+
+namespace {
+
+struct NormParams {
+    const void *x, *residual, *weight, *bias;
+    void *y, *s;
+    float *stats;
+    u64 ldx, ldr, ldy, lds;
+    u32 rows, cols, groups;         // groups of eight columns
+    float eps;
+    Mask mask;
+};
+
+struct NormBackParams {
+    const void *dy, *ds, *s, *weight;
+    const float *stats;
+    void *dres, *dx;
+    float *partial;                 // [workgroups][2][cols]: sums for dweight and dbias
+    u64 lddy, ldds, lds, lddres, lddx;
+    u32 rows, cols, groups;
+    Mask mask;
+};
+
+struct NormJoinParams {
+    const float *partial;
+    void *dweight, *dbias;
+    u32 parts, cols;
+};
+
+// The sums over the lanes that share a row: of a wavefront, or of the workgroup through `part`, which two
+// uses in a row must not share (the barrier between them lies in front of the second's reads).
+template <int LANES>
+DI float row_sum(float v, float *part)
+{
+    v = wave_sum(v);
+    if (LANES == 64) return v;
+    const u32 wave = wave_of_group();
+    if (lane_id() == 0) part[wave] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < LANES / 64; w++) v += part[w];
+    return v;
+}
+
+// s of eight columns: x, or residual + dropout(x)
+template <class T>
+DI void norm_input(const NormParams &p, u64 seed, u32 row, u32 group, float v[8])
+{
+    const u32 col = group * 8, n = p.cols - col;
+    load8((const T *)p.x + row * p.ldx + col, n, v);
+    if (p.residual) {
+        float r[8];
+        load8((const T *)p.residual + row * p.ldr + col, n, r);
+        if (p.mask.limit) drop8(p.mask, seed, row, group, v);
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] += r[i];
+    }
+}
+
+template <class T>
+DI void norm_output(const NormParams &p, u32 row, u32 group, const float v[8], float mean, float rstd)
+{
+    const u32 col = group * 8, n = p.cols - col;
+    float w[8], b[8], o[8];
+    if (p.weight) load8((const T *)p.weight + col, n, w);
+    if (p.bias) load8((const T *)p.bias + col, n, b);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        o[i] = (v[i] - mean) * rstd;
+        if (p.weight) o[i] *= w[i];
+        if (p.bias) o[i] += b[i];
+    }
+    store8((T *)p.y + row * p.ldy + col, n, o);
+    if (p.s) store8((T *)p.s + row * p.lds + col, n, v);
+}
+
+// Sum and squares around the mean of a row's part in a wavefront; `mine` columns, the other places hold 0.
+template <int LANES, int NG>
+DI void part_stats(const float v[NG][8], u32 lane, u32 cols, u32 mine, float *sum, float *m2)
+{
+    float a = 0.f, b = 0.f;
+#pragma unroll
+    for (int g = 0; g < NG; g++)
+#pragma unroll
+        for (int i = 0; i < 8; i++) a += v[g][i];
+    a = wave_sum(a);
+    const float mean = mine ? a / (float)mine : 0.f;
+#pragma unroll
+    for (int g = 0; g < NG; g++) {
+        const u32 col = (g * LANES + lane) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float d = v[g][i] - mean;
+            if (col + i < cols) b += d * d;
+        }
+    }
+    *sum = a;
+    *m2 = wave_sum(b);
+}
+
+// mean and 1 / sqrt(variance + eps) of a row from its parts
+template <int PARTS>
+DI void join_stats(const float *sum, const float *m2, const float *n, u32 cols, float eps, float *mean, float *rstd)
+{
+    float total = 0.f, squares = 0.f;
+#pragma unroll
+    for (int w = 0; w < PARTS; w++) total += sum[w];
+    *mean = total / (float)cols;
+#pragma unroll
+    for (int w = 0; w < PARTS; w++) {
+        const float d = n[w] > 0.f ? sum[w] / n[w] - *mean : 0.f;
+        squares += m2[w] + n[w] * d * d;
+    }
+    *rstd = 1.f / sqrtf(squares / (float)cols + eps);
+}
+
+// A row in the registers of LANES lanes, NG groups each; 64: four rows a workgroup.
+//
+// y goes by the sum s as it is in 32 bits.  The statistics for the backward pass are those of s rounded to the type,
+// which is what that pass reads: with the others a row of small variance, whose rstd is large, would get a gradient of
+// rounding errors, (s rounded - mean) * rstd.
+template <class T, int LANES, int NG>
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void norm_kernel(const NormParams p)
+{
+    const int PARTS = LANES / 64;
+    __shared__ float parts[2][5][PARTS];
+    const u32 lane = LANES == 64 ? lane_id() : threadIdx.x, wave = wave_of_group();
+    const u32 step = LANES == 64 ? gridDim.x * 4 : gridDim.x;
+    const bool rounded = sizeof(T) == 2 && p.s && p.stats;
+    u32 odd = 0;
+    const u64 seed = p.mask.limit ? mask_seed(p.mask) : 0;
+    // columns of this wavefront: those of the groups that its lanes have
+    const u32 first = LANES == 64 ? 0 : wave * 64;
+    u32 mine = 0;
+#pragma unroll
+    for (int g = 0; g < NG; g++) {
+        const u32 at = (g * LANES + first) * 8;
+        mine += p.cols > at ? min(p.cols - at, 512u) : 0u;
+    }
+    for (u32 row = LANES == 64 ? blockIdx.x * 4 + wave : blockIdx.x; row < p.rows; row += step) {
+        float v[NG][8];
+#pragma unroll
+        for (int g = 0; g < NG; g++) {
+            const u32 group = g * LANES + lane;
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[g][i] = 0.f;
+            if (group < p.groups) norm_input<T>(p, seed, row, group, v[g]);
+        }
+        float(&part)[5][PARTS] = parts[odd];        // two places in turn: a wavefront may be one row ahead, not two
+        odd ^= 1;
+        float sum, m2, n = (float)mine;
+        part_stats<LANES, NG>(v, lane, p.cols, mine, &sum, &m2);
+        if (PARTS > 1 && lane_id() == 0) {
+            part[0][wave] = sum;
+            part[1][wave] = m2;
+            part[2][wave] = n;
+        }
+        float sum2 = 0.f, m22 = 0.f;
+        if (rounded) {
+            float r[NG][8];
+#pragma unroll
+            for (int g = 0; g < NG; g++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) r[g][i] = (float)(T)v[g][i];
+            part_stats<LANES, NG>(r, lane, p.cols, mine, &sum2, &m22);
+            if (PARTS > 1 && lane_id() == 0) {
+                part[3][wave] = sum2;
+                part[4][wave] = m22;
+            }
+        }
+        float mean, rstd, mean2, rstd2;
+        if (PARTS > 1) {
+            __syncthreads();
+            join_stats<PARTS>(part[0], part[1], part[2], p.cols, p.eps, &mean, &rstd);
+        } else {
+            join_stats<1>(&sum, &m2, &n, p.cols, p.eps, &mean, &rstd);
+        }
+        if (p.stats && lane == 0) {
+            mean2 = mean;
+            rstd2 = rstd;
+            if (rounded) {
+                if (PARTS > 1)
+                    join_stats<PARTS>(part[3], part[4], part[2], p.cols, p.eps, &mean2, &rstd2);
+                else
+                    join_stats<1>(&sum2, &m22, &n, p.cols, p.eps, &mean2, &rstd2);
+            }
+            p.stats[(u64)row * 2] = mean2;
+            p.stats[(u64)row * 2 + 1] = rstd2;
+        }
+#pragma unroll
+        for (int g = 0; g < NG; g++) {
+            const u32 group = g * LANES + lane;
+            if (group < p.groups) norm_output<T>(p, row, group, v[g], mean, rstd);
+        }
+    }
+}
+
+// Rows that no workgroup's registers hold: read three times, the second and third time from a cache near by.
+template <class T>
+__global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p)
+{
+    __shared__ float part[4][16];
+    const u64 seed = p.mask.limit ? mask_seed(p.mask) : 0;
+    const bool rounded = sizeof(T) == 2 && p.s && p.stats;
+    for (u32 row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        float mean[2] = {}, m2[2] = {}, v[8];
+#pragma unroll
+        for (int pass = 0; pass < 2; pass++) {
+            float acc[2] = {};
+            for (u32 group = threadIdx.x; group < p.groups; group += 1024) {
+                norm_input<T>(p, seed, row, group, v);
+                const u32 n = p.cols - group * 8;
+                float one[2] = {};              // sums of sums: the rounding errors of a long row stay small
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float d = v[i] - mean[0], e = (float)(T)v[i] - mean[1];
+                    if ((u32)i < n) {
+                        one[0] += pass ? d * d : d;
+                        one[1] += pass ? e * e : e;
+                    }
+                }
+                acc[0] += one[0];
+                acc[1] += one[1];
+            }
+            float *const to = pass ? m2 : mean;
+            to[0] = row_sum<1024>(acc[0], part[pass * 2]) / (float)p.cols;
+            to[1] = row_sum<1024>(acc[1], part[pass * 2 + 1]) / (float)p.cols;
+        }
+        const float rstd = 1.f / sqrtf(m2[0] + p.eps);
+        if (p.stats && threadIdx.x == 0) {
+            p.stats[(u64)row * 2] = mean[rounded];
+            p.stats[(u64)row * 2 + 1] = 1.f / sqrtf(m2[rounded] + p.eps);
+        }
+        for (u32 group = threadIdx.x; group < p.groups; group += 1024) {
+            norm_input<T>(p, seed, row, group, v);
+            norm_output<T>(p, row, group, v, mean[0], rstd);
+        }
+    }
+}
+
+// What the gradient needs of eight columns: dy, the normalised input, and dy * weight
+template <class T>
+DI void back_input(const NormBackParams &p, u32 row, u32 group, float mean, float rstd, float dy[8], float h[8])
+{
+    const u32 col = group * 8, n = p.cols - col;
+    load8((const T *)p.dy + row * p.lddy + col, n, dy);
+    load8((const T *)p.s + row * p.lds + col, n, h);
+#pragma unroll
+    for (int i = 0; i < 8; i++) h[i] = (u32)i < n ? (h[i] - mean) * rstd : 0.f;
+}
+
+template <class T>
+DI void back_weight(const NormBackParams &p, u32 group, float w[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; i++) w[i] = 1.f;
+    if (p.weight) load8((const T *)p.weight + group * 8, p.cols - group * 8, w);
+}
+
+template <class T>
+DI void back_output(const NormBackParams &p, u64 seed, u32 row, u32 group, const float dy[8], const float h[8], const float w[8],
+                    float rstd, float c1, float c2)
+{
+    const u32 col = group * 8, n = p.cols - col;
+    float o[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) o[i] = rstd * (dy[i] * w[i] - c1 - h[i] * c2);
+    if (p.ds) {
+        float e[8];
+        load8((const T *)p.ds + row * p.ldds + col, n, e);
+#pragma unroll
+        for (int i = 0; i < 8; i++) o[i] += e[i];
+    }
+    store8((T *)p.dres + row * p.lddres + col, n, o);
+    if (p.dx) {
+        if (p.mask.limit) drop8(p.mask, seed, row, group, o);
+        store8((T *)p.dx + row * p.lddx + col, n, o);
+    }
+}
+
+// A workgroup takes every gridDim.x-th row (64 lanes: four rows at a time) and keeps the sums for the weights'
+// gradients in registers until its last row.
+template <class T, int LANES, int NG, bool WEIGHTS>
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void norm_back_kernel(const NormBackParams p)
+{
+    __shared__ float part[2][2][LANES / 64];
+    __shared__ float joined[LANES == 64 && WEIGHTS ? 4 * 64 * 8 : 1];
+    const u32 lane = LANES == 64 ? lane_id() : threadIdx.x;
+    const u32 first = LANES == 64 ? blockIdx.x * 4 + wave_of_group() : blockIdx.x;
+    const u32 step = LANES == 64 ? gridDim.x * 4 : gridDim.x;
+    const u64 seed = p.mask.limit ? mask_seed(p.mask) : 0;
+    float w[NG][8], dw[WEIGHTS ? NG : 1][8], db[WEIGHTS ? NG : 1][8];
+#pragma unroll
+    for (int g = 0; g < NG; g++) {
+        const u32 group = g * LANES + lane;
+        if (group < p.groups) back_weight<T>(p, group, w[g]);
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (WEIGHTS) dw[g][i] = db[g][i] = 0.f;
+    }
+    u32 odd = 0;
+    for (u32 row = first; row < p.rows; row += step) {
+        const float mean = p.stats[(u64)row * 2], rstd = p.stats[(u64)row * 2 + 1];
+        float dy[NG][8], h[NG][8];
+        float c1 = 0.f, c2 = 0.f;
+#pragma unroll
+        for (int g = 0; g < NG; g++) {
+            const u32 group = g * LANES + lane;
+#pragma unroll
+            for (int i = 0; i < 8; i++) dy[g][i] = h[g][i] = 0.f;
+            if (group < p.groups) {
+                back_input<T>(p, row, group, mean, rstd, dy[g], h[g]);
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float e = dy[g][i] * w[g][i];
+                    c1 += e;
+                    c2 += e * h[g][i];
+                    if (WEIGHTS) {
+                        dw[g][i] += dy[g][i] * h[g][i];
+                        db[g][i] += dy[g][i];
+                    }
+                }
+            }
+        }
+        c1 = wave_sum(c1);
+        c2 = wave_sum(c2);
+        if (LANES > 64) {           // two places in turn: a wavefront may be one row ahead, not two
+            if (lane_id() == 0) {
+                part[odd][0][wave_of_group()] = c1;
+                part[odd][1][wave_of_group()] = c2;
+            }
+            __syncthreads();
+            c1 = c2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < LANES / 64; i++) {
+                c1 += part[odd][0][i];
+                c2 += part[odd][1][i];
+            }
+            odd ^= 1;
+        }
+        c1 /= (float)p.cols;
+        c2 /= (float)p.cols;
+#pragma unroll
+        for (int g = 0; g < NG; g++) {
+            const u32 group = g * LANES + lane;
+            if (group < p.groups) back_output<T>(p, seed, row, group, dy[g], h[g], w[g], rstd, c1, c2);
+        }
+    }
+    if (WEIGHTS) {
+        float *out = p.partial + (u64)blockIdx.x * 2 * p.cols;
+#pragma unroll
+        for (int g = 0; g < NG; g++) {
+            const u32 group = g * LANES + lane;
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                float(&v)[8] = k ? db[g] : dw[g];
+                if (LANES == 64) {      // the four wavefronts' sums
+                    __syncthreads();
+#pragma unroll
+                    for (int i = 0; i < 8; i++) joined[(wave_of_group() * 8 + i) * 64 + lane] = v[i];
+                    __syncthreads();
+#pragma unroll
+                    for (int i = 0; i < 8; i++) {
+                        v[i] = 0.f;
+#pragma unroll
+                        for (int u = 0; u < 4; u++) v[i] += joined[(u * 8 + i) * 64 + lane];
+                    }
+                    if (wave_of_group() != 0) continue;
+                }
+                if (group < p.groups) store8(out + (u64)k * p.cols + group * 8, p.cols - group * 8, v);
+            }
+        }
+    }
+}
+
+// Rows that no workgroup's registers hold: two passes over dy and s, the weights' sums in the workgroup's place in memory,
+// where each column belongs to one lane.
+template <class T, bool WEIGHTS>
+__global__ __launch_bounds__(1024) void norm_back_long_kernel(const NormBackParams p)
+{
+    __shared__ float part[4][16];
+    const u64 seed = p.mask.limit ? mask_seed(p.mask) : 0;
+    float *const dw = WEIGHTS ? p.partial + (u64)blockIdx.x * 2 * p.cols : nullptr;
+    float dy[8], h[8], w[8];
+    u32 odd = 0;
+    bool begun = false;
+    for (u32 row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const float mean = p.stats[(u64)row * 2], rstd = p.stats[(u64)row * 2 + 1];
+        float c1 = 0.f, c2 = 0.f;
+        for (u32 group = threadIdx.x; group < p.groups; group += 1024) {
+            back_input<T>(p, row, group, mean, rstd, dy, h);
+            back_weight<T>(p, group, w);
+            float e1 = 0.f, e2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                e1 += dy[i] * w[i];
+                e2 += dy[i] * w[i] * h[i];
+            }
+            c1 += e1;
+            c2 += e2;
+            if (WEIGHTS) {
+                const u32 n = p.cols - group * 8;
+                float a[8] = {}, b[8] = {};
+                if (begun) {
+                    load8(dw + group * 8, n, a);
+                    load8(dw + p.cols + group * 8, n, b);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    a[i] += dy[i] * h[i];
+                    b[i] += dy[i];
+                }
+                store8(dw + group * 8, n, a);
+                store8(dw + p.cols + group * 8, n, b);
+            }
+        }
+        begun = true;
+        c1 = row_sum<1024>(c1, part[odd]) / (float)p.cols;
+        c2 = row_sum<1024>(c2, part[odd + 1]) / (float)p.cols;
+        odd ^= 2;
+        for (u32 group = threadIdx.x; group < p.groups; group += 1024) {
+            back_input<T>(p, row, group, mean, rstd, dy, h);
+            back_weight<T>(p, group, w);
+            back_output<T>(p, seed, row, group, dy, h, w, rstd, c1, c2);
+        }
+    }
+}
+
+// dweight and dbias from the workgroups' sums: 32 columns a workgroup, its eight rows of lanes take every eighth part
+template <class T>
+__global__ __launch_bounds__(256) void norm_join_kernel(const NormJoinParams p)
+{
+    __shared__ float sums[8][33];
+    const u32 x = threadIdx.x & 31, y = threadIdx.x >> 5, k = blockIdx.y;
+    T *const out = (T *)(k ? p.dbias : p.dweight);
+    const u32 col = blockIdx.x * 32 + x;
+    float v = 0.f;
+    if (out && col < p.cols)
+        for (u32 i = y; i < p.parts; i += 8) v += p.partial[((u64)i * 2 + k) * p.cols + col];
+    sums[y][x] = v;
+    __syncthreads();
+    if (y == 0 && out && col < p.cols) {
+#pragma unroll
+        for (int i = 1; i < 8; i++) v += sums[i][x];
+        out[col] = (T)v;
+    }
+}
+
+template <class T>
+int launch_norm(const NormParams &p, void *stream)
+{
+    const u32 g = p.groups, most = 1u << 18;      // workgroups; they go on to further rows
+    const dim3 quarter(p.rows / 4 < most ? (p.rows + 3) / 4 : most), each(p.rows < most ? p.rows : most);
+    if (g <= 64) return ops_launch(norm_kernel<T, 64, 1>, quarter, dim3(256), 0, p, stream);
+    if (g <= 128) return ops_launch(norm_kernel<T, 64, 2>, quarter, dim3(256), 0, p, stream);
+    if (g <= 256) return ops_launch(norm_kernel<T, 256, 1>, each, dim3(256), 0, p, stream);
+    if (g <= 512) return ops_launch(norm_kernel<T, 256, 2>, each, dim3(256), 0, p, stream);
+    if (g <= 1024) return ops_launch(norm_kernel<T, 256, 4>, each, dim3(256), 0, p, stream);
+    if (g <= 2048) return ops_launch(norm_kernel<T, 1024, 2>, each, dim3(1024), 0, p, stream);
+    if (g <= 4096) return ops_launch(norm_kernel<T, 1024, 4>, each, dim3(1024), 0, p, stream);
+    return ops_launch(norm_long_kernel<T>, each, dim3(1024), 0, p, stream);
+}
+
+template <class T, bool WEIGHTS>
+int launch_norm_back(const NormBackParams &p, u32 grid, void *stream)
+{
+    const u32 g = p.groups;
+    if (g <= 64) return ops_launch(norm_back_kernel<T, 64, 1, WEIGHTS>, dim3(grid), dim3(256), 0, p, stream);
+    if (g <= 128) return ops_launch(norm_back_kernel<T, 64, 2, WEIGHTS>, dim3(grid), dim3(256), 0, p, stream);
+    if (g <= 256) return ops_launch(norm_back_kernel<T, 256, 1, WEIGHTS>, dim3(grid), dim3(256), 0, p, stream);
+    if (g <= 512) return ops_launch(norm_back_kernel<T, 256, 2, WEIGHTS>, dim3(grid), dim3(256), 0, p, stream);
+    if (g <= 1024) return ops_launch(norm_back_kernel<T, 512, 2, WEIGHTS>, dim3(grid), dim3(512), 0, p, stream);
+    if (g <= 2048) return ops_launch(norm_back_kernel<T, 1024, 2, WEIGHTS>, dim3(grid), dim3(1024), 0, p, stream);
+    return ops_launch(norm_back_long_kernel<T, WEIGHTS>, dim3(grid), dim3(1024), 0, p, stream);
+}
+
+bool wants_weights(const vms_layernorm_backward_args *a) { return a->d_dweight || a->d_dbias; }
+
+// workgroups of the backward pass: as many as are resident at once, each with sums of its own to be joined
+u32 back_grid(u64 rows, u64 cols)
+{
+    const u64 groups = (cols + 7) / 8;
+    const u64 blocks = groups <= 128 ? (rows + 3) / 4 : rows;
+    const u64 most = groups <= 512 ? OPS_CUS * 4 : groups <= 1024 ? OPS_CUS * 2 : OPS_CUS;
+    return (u32)(blocks < most ? blocks : most);
+}
+
+}  // namespace
+
+extern "C" int vms_layernorm(const vms_layernorm_args *a, void *stream)
+{
+    if (!a) return VMS_EINVAL;
+    if (a->struct_size != sizeof *a) return VMS_ESTRUCT;
+    NormParams p;
+    int rc = make_mask(a->mask, &p.mask);
+    if (rc) return rc;
+    if (a->dtype > VMS_BF16 || a->rows >> 31 || a->cols >> 31 || !a->cols || !(a->eps >= 0.0)) return VMS_EINVAL;
+    if (!a->rows) return VMS_OK;
+    if (!input_ok(a->d_x, a->dtype) || !output_ok(a->d_y, a->dtype, a->ldy, a->cols)) return VMS_EINVAL;
+    if (a->d_residual ? !input_ok(a->d_residual, a->dtype) : a->mask.p > 0.0 || a->d_s) return VMS_EINVAL;
+    if (a->d_s && !output_ok(a->d_s, a->dtype, a->lds, a->cols)) return VMS_EINVAL;
+    if ((a->d_weight && !input_ok(a->d_weight, a->dtype)) || (a->d_bias && !input_ok(a->d_bias, a->dtype))) return VMS_EINVAL;
+    if ((uintptr_t)a->d_stats % 4) return VMS_EINVAL;
+    if (!stride_ok(a->ldx) || !stride_ok(a->ldr) || !stride_ok(a->ldy) || !stride_ok(a->lds)) return VMS_EINVAL;
+    p.x = a->d_x;
+    p.residual = a->d_residual;
+    p.weight = a->d_weight;
+    p.bias = a->d_bias;
+    p.y = a->d_y;
+    p.s = a->d_s;
+    p.stats = a->d_stats;
+    p.ldx = a->ldx;
+    p.ldr = a->ldr;
+    p.ldy = a->ldy;
+    p.lds = a->lds;
+    p.rows = (u32)a->rows;
+    p.cols = (u32)a->cols;
+    p.groups = (p.cols + 7) / 8;
+    p.eps = (float)a->eps;
+    return with_type(a->dtype, [&](auto *t) { return launch_norm<std::remove_pointer_t<decltype(t)>>(p, stream); });
+}
+
+extern "C" size_t vms_layernorm_backward_workspace_bytes(const vms_layernorm_backward_args *a)
+{
+    if (!a || a->struct_size != sizeof *a || a->rows >> 31 || a->cols >> 31 || !wants_weights(a)) return 0;
+    return (size_t)back_grid(a->rows, a->cols) * 2 * a->cols * sizeof(float);
+}
+
+extern "C" int vms_layernorm_backward(const vms_layernorm_backward_args *a, void *stream)
+{
+    if (!a) return VMS_EINVAL;
+    if (a->struct_size != sizeof *a) return VMS_ESTRUCT;
+    NormBackParams p;
+    int rc = make_mask(a->mask, &p.mask);
+    if (rc) return rc;
+    if (a->dtype > VMS_BF16 || a->rows >> 31 || a->cols >> 31 || !a->cols) return VMS_EINVAL;
+    const bool weights = wants_weights(a);
+    for (const void *d : { a->d_dweight, a->d_dbias })
+        if (d && !input_ok(d, a->dtype)) return VMS_EINVAL;
+    if (a->rows) {
+        if (!input_ok(a->d_dy, a->dtype) || !input_ok(a->d_s, a->dtype) || !output_ok(a->d_dres, a->dtype, a->lddres, a->cols)) return VMS_EINVAL;
+        if ((a->d_ds && !input_ok(a->d_ds, a->dtype)) || (a->d_weight && !input_ok(a->d_weight, a->dtype))) return VMS_EINVAL;
+        if (a->d_dx && !output_ok(a->d_dx, a->dtype, a->lddx, a->cols)) return VMS_EINVAL;
+        if (!a->d_stats || (uintptr_t)a->d_stats % 4) return VMS_EINVAL;
+        if (!stride_ok(a->lddy) || !stride_ok(a->ldds) || !stride_ok(a->lds) || !stride_ok(a->lddres) || !stride_ok(a->lddx)) return VMS_EINVAL;
+        const size_t need = vms_layernorm_backward_workspace_bytes(a);
+        if (need && (!a->d_workspace || (uintptr_t)a->d_workspace % 16 || a->workspace_bytes < need)) return VMS_EWORKSPACE;
+    }
+    p.dy = a->d_dy;
+    p.ds = a->d_ds;
+    p.s = a->d_s;
+    p.weight = a->d_weight;
+    p.stats = a->d_stats;
+    p.dres = a->d_dres;
+    p.dx = a->d_dx;
+    p.partial = (float *)a->d_workspace;
+    p.lddy = a->lddy;
+    p.ldds = a->ldds;
+    p.lds = a->lds;
+    p.lddres = a->lddres;
+    p.lddx = a->lddx;
+    p.rows = (u32)a->rows;
+    p.cols = (u32)a->cols;
+    p.groups = (p.cols + 7) / 8;
+    const u32 grid = back_grid(a->rows, a->cols);
+    return with_type(a->dtype, [&](auto *t) {
+        typedef std::remove_pointer_t<decltype(t)> T;
+        if (a->rows) {
+            rc = weights ? launch_norm_back<T, true>(p, grid, stream) : launch_norm_back<T, false>(p, grid, stream);
+            if (rc) return rc;
+        }
+        if (!weights) return (int)VMS_OK;
+        const NormJoinParams j = { (const float *)a->d_workspace, a->d_dweight, a->d_dbias, grid, p.cols };
+        return ops_launch(norm_join_kernel<T>, dim3((p.cols + 31) / 32, 2), dim3(256), 0, j, stream);
+    });
+}
