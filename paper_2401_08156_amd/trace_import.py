@@ -17,6 +17,7 @@ of a live key cannot be replayed and are counted, not emitted.
 
     python -m paper_2401_08156_amd.trace_import --text trace.txt     # replay a text recording
     python -m paper_2401_08156_amd.trace_import --record             # record a small PyTorch loop, replay it
+    python -m paper_2401_08156_amd.trace_import --record --strategy LR --dropout 0.1    # with LoRA and recomputation
 """
 import argparse
 import heapq
@@ -153,19 +154,24 @@ def replay(events, max_slots, **overrides):
     return out
 
 
-def _demo_loop(steps=12, hidden=1024, layers=6):
+def _demo_loop(steps=12, hidden=1024, layers=6, **strategy):
     from .torch_plugin import train
-    train(steps, hidden, layers)
+    train(steps, hidden, layers, **strategy)
 
 
 def main():
+    from .torch_plugin import add_strategy_options, strategy_options
     ap = argparse.ArgumentParser()
     ap.add_argument("--text", help="replay a text recording (alloc <key> <bytes> / free <key> per line)")
     ap.add_argument("--record", action="store_true", help="record a small PyTorch training loop on the GPU and replay it")
     ap.add_argument("--save", help="with --record: also write the recording as text")
+    add_strategy_options(ap)
     args = ap.parse_args()
+    strategy = strategy_options(ap, args)
+    if args.strategy and not args.record:
+        ap.error("--strategy needs --record")
     if args.record:
-        records, peaks = record_torch_loop(_demo_loop)
+        records, peaks = record_torch_loop(lambda: _demo_loop(**strategy))
         if args.save:
             records_to_text(records, args.save)
     elif args.text:

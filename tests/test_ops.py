@@ -232,3 +232,17 @@ def test_rows_of_any_strides(make, same, stride):
     rows, cols = ops._rows(t)
     flat = torch.as_strided(m, (rows, cols), (ld, 1), m.storage_offset())
     assert torch.equal(flat, t.reshape(rows, cols)) and flat.shape == t.reshape(rows, cols).shape
+
+
+@pytest.mark.parametrize("module,argv", [
+    ("torch_plugin", ["--dropout", "0.1"]), ("torch_plugin", ["--strategy", "X"]), ("torch_plugin", ["--strategy", "N", "--dropout", "2"]),
+    ("torch_plugin", ["--strategy", "L", "--rank", "0"]), ("trace_import", ["--text", "nothing.txt", "--strategy", "L"]),
+    ("trace_import", ["--record", "--dropout", "0.5"]),
+])
+def test_the_commands_refuse_options_that_do_not_go_together(module, argv, monkeypatch, capsys):
+    import importlib
+    import sys
+    monkeypatch.setattr(sys, "argv", [module] + argv)
+    with pytest.raises(SystemExit) as e:
+        importlib.import_module("paper_2401_08156_amd." + module).main()
+    assert e.value.code == 2 and "--" in capsys.readouterr().err
