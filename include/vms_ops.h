@@ -115,8 +115,10 @@ int vms_layernorm_backward(const vms_layernorm_backward_args *a, void *stream);
  * d_starts = NULL: all rows are one request of adapter 0.
  * d_y = d_out (same stride): the sum is made in place, and rows of no request are not touched.
  *
- * d_hidden (vms_lowrank_hidden_bytes, 16-byte aligned) receives scale * x a^T in 32 bits: workspace of
- * the forward pass, and what the backward pass reads.                                             */
+ * d_hidden (vms_lowrank_hidden_bytes, 16-byte aligned) receives scale * x a^T: workspace of the forward
+ * pass, and what the backward pass reads.  In a layout of the library's own, rounded to the type (a
+ * value that float16 does not hold becomes an infinity there, as it does in a program that stores it),
+ * or as sums in parts.                                                                            */
 #define VMS_LOWRANK_MAX_RANK 128
 typedef struct vms_lowrank_args {
     uint32_t struct_size;        /* sizeof(vms_lowrank_args)                                        */
@@ -130,8 +132,8 @@ typedef struct vms_lowrank_args {
     const void *d_x, *d_y, *d_a, *d_b;      /* a and b without gaps                                 */
     const int32_t *d_starts, *d_which;
     void *d_out;
-    uint64_t ldx, ldy, ldo;
-    float *d_hidden;
+    uint64_t ldx, ldy, ldo;      /* each below 2^23, here and in the backward pass                  */
+    void *d_hidden;
     uint64_t hidden_bytes;
 } vms_lowrank_args;
 size_t vms_lowrank_hidden_bytes(const vms_lowrank_args *a);             /* reads the sizes only; 0 if they are wrong */

@@ -126,6 +126,14 @@ DI void drop8(const Mask &m, u64 seed, u32 row, u32 group, float v[8])
     }
 }
 
+// Workgroups go to the eight dies in turn, and each die has a cache of its own.  Where neighbours of a grid share memory
+// lines or walk through neighbouring ones, they are numbered so that a die gets a run of them: the b-th of n.
+DI u32 die_order(u32 b, u32 n)
+{
+    const u32 die = b % 8, each = n / 8, more = n % 8;
+    return die * each + min(die, more) + b / 8;
+}
+
 const u32 OPS_CUS = 256;        // compute units of the device that the grids are sized for
 
 template <class P>

@@ -1,16 +1,19 @@
 // vms_lowrank and vms_lowrank_backward (include/vms_ops.h): out = y + scale (x a^T) b^T, an adapter for each request.
 //
 // With ranks of some tens every product here does 2 rank operations per element of x, y or dout that it moves, a tenth of
-// what the matrix units could do in that time: all kernels are bound by memory, and the tiles are laid out so that each of
-// the wide tensors is read once, 16 bytes a lane, straight into the operand registers of the matrix instructions:
-//   down    hidden = scale x a^T     rows of x and of a are both consecutive in the summed dimension
-//   up      out = y + hidden b^T     hidden in registers for all columns, the products transposed so that a lane ends up
-//                                    with 16 bytes of consecutive columns of one row
+// what the matrix units could do in that time: all kernels are bound by memory, and each of the wide tensors is read once,
+// straight into the operand registers of the matrix instructions:
+//   down    hidden = scale x a^T     summed along the rows of x and of a
+//   up      out = y + hidden b^T     a panel of b in the LDS for all rows of a tile
 //   outer   da = dhidden^T x, db = dout^T hidden, summed over rows: a lane reads some columns of eight rows and swaps
 //                                    them in its own registers
 // The forward pass is down and up; the backward pass is down on dout with b transposed, up with a transposed, and outer
-// twice.  An order of the summed elements is the same for both operands of a product, so any order will do; the lanes'
-// loads decide it.
+// twice.  The order of the summed elements is the same for both operands of a product, so any order will do.
+//
+// The operands want a row in each of 16 neighbouring lanes, the memory path 64 consecutive bytes in each four: taken as the
+// operands want them, loads of 16 bytes a lane go through the address unit one lane at a time (64 accesses an instruction by
+// its counter; the unit was busy for three quarters of the time, at 2 TB/s).  So four loads take four rows of 256 bytes
+// each, and four neighbouring lanes swap their four registers (quad_swap).
 #include "ops_common.hpp"
 
 namespace {
@@ -54,6 +57,37 @@ DI typename Some<T, N>::type load_first(const T *p, int n)
     for (int i = 0; i < N; i++) v[i] = i < n ? p[i] : (T)0.f;
     return v;
 }
+
+// The lanes of a quad swap their registers: lane c's r[i] becomes lane i's r[c]
+template <class V>
+DI void quad_swap(V r[4])
+{
+    u32 v[4][4];
+    __builtin_memcpy(v, r, sizeof v);
+    const bool odd = threadIdx.x & 1, upper = threadIdx.x & 2;
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            const u32 a = dpp_perm<DPP_QUAD_XOR1>(v[i][k]), b = dpp_perm<DPP_QUAD_XOR1>(v[i + 1][k]);
+            v[i][k] = odd ? b : v[i][k];
+            v[i + 1][k] = odd ? v[i + 1][k] : a;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const u32 a = dpp_perm<DPP_QUAD_XOR2>(v[i][k]), b = dpp_perm<DPP_QUAD_XOR2>(v[i + 2][k]);
+            v[i][k] = upper ? b : v[i][k];
+            v[i + 2][k] = upper ? v[i + 2][k] : a;
+        }
+    }
+    __builtin_memcpy(r, v, sizeof v);
+}
+
+// The same four rows of 256 bytes in a lane's terms: before a swap, register u of lane 16 group + 4 quad + c is bytes
+// 64 group + 16 c of row 4 quad + u; after it, of row 4 quad + c it has bytes 64 group + 16 u.
+const int SLAB_BYTES = 256;
+DI u32 slab_row(u32 lane, int u) { return (lane >> 2 & 3) * 4 + u; }
+DI u32 slab_byte(u32 lane) { return (lane >> 4) * 64 + (lane & 3) * 16; }
 
 struct Requests {
     const int32_t *starts, *which;
@@ -113,76 +147,132 @@ DI bool find_tile(const Requests &q, u32 tile, Tile *out)
 
 // ---- down: hidden[row][j] = scale sum_k x[row][k] w[j][k] ------------------------------------------------------------
 
+// What a batch's hidden values are kept as.  Whole sums are rounded to the type of the tensors, as the products that read
+// them take them: half a step of the type for each term of a sum over the rank.  They are laid out twice, in the order in
+// which the lanes of `up` and of `outer` read them, padded to 16 rows.  Where there are not tiles enough for the compute
+// units, workgroups share the summed dimension and leave parts of the sums, in 32 bits: [splits][rows][padded].
+struct Hidden {
+    void *up;                   // [rows / 16][padded / EPL][16][EPL]
+    void *outer;                // 16 bits: [rows / 8][padded][8]; 32 bits: [rows][padded]
+    float *parts;               // not null: what `down` leaves
+    u32 splits, padded;
+    bool folded;                // the parts are put together in `up` and `outer` before they are read
+};
+
+template <class T>
+DI u64 up_place(u64 row, u32 j, u32 padded)
+{
+    const u32 EPL = Mma<T>::EPL;
+    return (row >> 4) * 16 * padded + j / EPL * (16 * EPL) + (row & 15) * EPL + j % EPL;
+}
+template <class T>
+DI u64 outer_place(u64 row, u32 j, u32 padded)
+{
+    return sizeof(T) == 4 ? row * padded + j : ((row >> 3) * padded + j) * 8 + (row & 7);
+}
+
+// four values of a row, from column `col` of the rank on
+template <class T>
+DI void store_hidden(const Hidden &h, const f32x4 &v, u64 row, u32 col, u32 split, u64 rows)
+{
+    if (h.parts) {
+        *(f32x4 *)(h.parts + (split * rows + row) * h.padded + col) = v;
+        return;
+    }
+    typename Some<T, 4>::type o;
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] = (T)v[e];
+    *(typename Some<T, 4>::type *)((T *)h.up + up_place<T>(row, col, h.padded)) = o;
+#pragma unroll
+    for (int e = 0; e < 4; e++) ((T *)h.outer)[outer_place<T>(row, col + e, h.padded)] = o[e];
+}
+
 struct DownParams {
     const void *x, *w;          // w [adapters][rank][in]
-    float *hidden;              // [splits][rows][NR * 16], zeros behind the rank
+    Hidden h;
     const float *scales;
     Requests q;
     u64 ldx;
     float scale;
-    u32 in, rank, splits;
+    u32 in, rank;
 };
 
-// STEPS steps of the summed dimension, all loads in front
-template <class T, int MR, int NR, int STEPS>
-DI void down_steps(const T *const x[MR], const T *const w[NR], u32 s, f32x4 acc[MR][NR])
+// One slab of the summed dimension: 256 bytes of each row, of which `n` elements exist (WHOLE: all)
+template <class T, int MR, int NR, bool WHOLE>
+DI void down_slab(const char *x, const char *w, const u32 (&xat)[MR][4], const u32 (&wat)[NR][4], int n, f32x4 (&acc)[MR][NR])
 {
     typedef typename Mma<T>::Frag Frag;
-    const int EPL = Mma<T>::EPL, STEP = Mma<T>::STEP;
-    Frag a[STEPS][MR], b[STEPS][NR];
+    const int EPL = Mma<T>::EPL;
+    const int SOME = NR < 4 ? NR : 4;       // of the rank's parts at a time; the registers do not hold more
+    Frag a[MR][4], b[SOME][4];
+    n -= (int)(slab_byte(lane_id()) / sizeof(T));
+    const auto load = [n](const char *p, u32 at) { return WHOLE ? load_some<EPL>((const T *)(p + at)) : load_first<EPL>((const T *)(p + at), n); };
 #pragma unroll
-    for (int k = 0; k < STEPS; k++) {
+    for (int i = 0; i < MR; i++)
 #pragma unroll
-        for (int i = 0; i < MR; i++) a[k][i] = load_some<EPL>(x[i] + (u64)(s + k) * STEP);
+        for (int u = 0; u < 4; u++) a[i][u] = load(x, xat[i][u]);
 #pragma unroll
-        for (int j = 0; j < NR; j++) b[k][j] = load_some<EPL>(w[j] + (u64)(s + k) * STEP);
+    for (int from = 0; from < NR; from += SOME) {
+#pragma unroll
+        for (int j = 0; j < SOME; j++)
+#pragma unroll
+            for (int u = 0; u < 4; u++) b[j][u] = load(w, wat[from + j][u]);
+        // (loads in front of the swaps, and those one after the other: mixed freely they take more registers than there are)
+        __builtin_amdgcn_sched_barrier(0);
+        if (from == 0) {
+#pragma unroll
+            for (int i = 0; i < MR; i++) {
+                quad_swap(a[i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < SOME; j++) {
+            quad_swap(b[j]);
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+#pragma unroll
+                for (int i = 0; i < MR; i++) acc[i][from + j] = mma(b[j][u], a[i][u], acc[i][from + j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
-#pragma unroll
-    for (int k = 0; k < STEPS; k++)
-#pragma unroll
-        for (int i = 0; i < MR; i++)
-#pragma unroll
-            for (int j = 0; j < NR; j++) acc[i][j] = mma(b[k][j], a[k][i], acc[i][j]);
 }
 
-// MR x 16 rows and the whole rank in a workgroup; its four wavefronts, and `splits` workgroups, share the summed dimension.
-template <class T, int MR, int NR>
-__global__ __launch_bounds__(256) void lowrank_down_kernel(const DownParams p)
+// MR x 16 rows and the whole rank in a workgroup; its WAVES wavefronts, and `splits` workgroups, share the summed dimension.
+template <class T, int MR, int NR, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void lowrank_down_kernel(const DownParams p)
 {
-    typedef typename Mma<T>::Frag Frag;
-    const int EPL = Mma<T>::EPL, STEP = Mma<T>::STEP, AT_ONCE = 2;
-    __shared__ f32x4 part[4][NR][64];
+    const u32 SLAB = SLAB_BYTES / sizeof(T);
+    __shared__ f32x4 part[WAVES][NR][64];
     Tile t;
     if (!find_tile<MR * 16>(p.q, blockIdx.x, &t) || t.adapter < 0) return;
-    const u32 lane = lane_id(), m = lane & 15, group = lane >> 4, wave = wave_of_group();
-    const T *x[MR], *w[NR];     // rows beyond the tile and the rank are the last one again: their results go nowhere
+    const u32 lane = lane_id(), wave = wave_of_group();
+    const char *const x = (const char *)((const T *)p.x + t.row * p.ldx);
+    const char *const w = (const char *)((const T *)p.w + (u64)t.adapter * p.rank * p.in);
+    u32 xat[MR][4], wat[NR][4];     // rows beyond the tile and the rank are the last one again: their results go nowhere
 #pragma unroll
-    for (int i = 0; i < MR; i++) x[i] = (const T *)p.x + (t.row + min(i * 16 + m, t.rows - 1)) * p.ldx + group * EPL;
+    for (int u = 0; u < 4; u++) {
 #pragma unroll
-    for (int j = 0; j < NR; j++) w[j] = (const T *)p.w + ((u64)t.adapter * p.rank + min(j * 16 + m, p.rank - 1)) * p.in + group * EPL;
+        for (int i = 0; i < MR; i++) xat[i][u] = min(i * 16 + slab_row(lane, u), t.rows - 1) * (u32)p.ldx * (u32)sizeof(T) + slab_byte(lane);
+#pragma unroll
+        for (int j = 0; j < NR; j++) wat[j][u] = min(j * 16 + slab_row(lane, u), p.rank - 1) * p.in * (u32)sizeof(T) + slab_byte(lane);
+    }
     f32x4 acc[MR][NR];
 #pragma unroll
     for (int i = 0; i < MR; i++)
 #pragma unroll
         for (int j = 0; j < NR; j++) acc[i][j] = f32x4{ 0.f, 0.f, 0.f, 0.f };
 
-    const u32 steps = p.in / STEP, shares = p.splits * 4, share = blockIdx.y * 4 + wave;
-    const u32 first = (u32)((u64)steps * share / shares), last = (u32)((u64)steps * (share + 1) / shares);
-    u32 s = first;
-    for (; s + AT_ONCE <= last; s += AT_ONCE) down_steps<T, MR, NR, AT_ONCE>(x, w, s, acc);
-    for (; s < last; s++) down_steps<T, MR, NR, 1>(x, w, s, acc);
-    if (share == shares - 1 && steps * STEP < p.in) {
-        const int n = (int)(p.in - steps * STEP) - (int)group * EPL;
-        Frag b[NR];
-#pragma unroll
-        for (int j = 0; j < NR; j++) b[j] = load_first<EPL>(w[j] + (u64)steps * STEP, n);
-#pragma unroll
-        for (int i = 0; i < MR; i++) {
-            const Frag a = load_first<EPL>(x[i] + (u64)steps * STEP, n);
-#pragma unroll
-            for (int j = 0; j < NR; j++) acc[i][j] = mma(b[j], a, acc[i][j]);
-        }
+    // A wavefront takes a slab and leaves the next ones to the others.  Tiles begin at different places: rows are often a
+    // power of two apart, so that what all tiles read at one place is in one channel of the caches.
+    const u32 slabs = p.in / SLAB, shares = p.h.splits * WAVES, share = blockIdx.y * WAVES + wave;
+    const u32 turn = slabs ? blockIdx.x * WAVES % slabs : 0;
+    for (u32 s = share; s < slabs; s += shares) {
+        const u64 at = (u64)(s + turn < slabs ? s + turn : s + turn - slabs) * SLAB_BYTES;
+        down_slab<T, MR, NR, true>(x + at, w + at, xat, wat, 0, acc);
     }
+    if (share == shares - 1 && slabs * SLAB < p.in)
+        down_slab<T, MR, NR, false>(x + (u64)slabs * SLAB_BYTES, w + (u64)slabs * SLAB_BYTES, xat, wat, (int)(p.in - slabs * SLAB), acc);
 
     const float scale = p.scales ? p.scales[t.adapter] : p.scale;
 #pragma unroll
@@ -191,116 +281,326 @@ __global__ __launch_bounds__(256) void lowrank_down_kernel(const DownParams p)
 #pragma unroll
         for (int j = 0; j < NR; j++) part[wave][j][lane] = acc[i][j];
         __syncthreads();
-        for (u32 at = threadIdx.x; at < NR * 64; at += 256) {
+        for (u32 at = threadIdx.x; at < NR * 64; at += WAVES * 64) {
             const u32 j = at >> 6, l = at & 63, row = i * 16 + (l & 15), col = j * 16 + (l >> 4) * 4;
             f32x4 v = part[0][j][l];
 #pragma unroll
-            for (int u = 1; u < 4; u++)
+            for (int u = 1; u < WAVES; u++)
 #pragma unroll
                 for (int e = 0; e < 4; e++) v[e] += part[u][j][l][e];
 #pragma unroll
             for (int e = 0; e < 4; e++) v[e] = col + e < p.rank ? v[e] * scale : 0.f;
-            if (row < t.rows) *(f32x4 *)(p.hidden + (((u64)blockIdx.y * p.q.rows + t.row + row) * NR * 16 + col)) = v;
+            if (row < t.rows) store_hidden<T>(p.h, v, t.row + row, col, blockIdx.y, p.q.rows);
         }
     }
+}
+
+// The same for long requests and ranks above 32.  There the weights, read once for 32 rows, are two thirds of what goes
+// through the vector cache, whose requests in flight are what bounds the kernel above (110 lines a compute unit, 0.98 us each,
+// 2.9 TB/s of x).  Here four wavefronts with 32 rows each share them in the LDS, a slab for each half of the workgroup at a
+// time, and the next slabs are on their way meanwhile.
+template <class T, int NR>
+__global__ __launch_bounds__(512) void lowrank_down_shared_kernel(const DownParams p)
+{
+    typedef typename Mma<T>::Frag Frag;
+    const int EPL = Mma<T>::EPL, MR = 2, CHUNKS = NR * 16 * 16, FILL = CHUNKS / 256;
+    const u32 SLAB = SLAB_BYTES / sizeof(T);
+    __shared__ Frag panel[2][2][CHUNKS];        // 16 chunks of 16 bytes for each of NR * 16 rows of w
+    Tile t;
+    if (!find_tile<128>(p.q, blockIdx.x, &t) || t.adapter < 0) return;
+    const u32 lane = lane_id(), m = lane & 15, group = lane >> 4, wave = wave_of_group(), mine = wave >> 2, local = threadIdx.x & 255;
+    const u32 first = (wave & 3) * 32, rows = t.rows > first ? t.rows - first : 0, last = rows ? rows - 1 : 0;
+    const char *const x = (const char *)((const T *)p.x + (t.row + (rows ? first : 0)) * p.ldx);
+    const char *const w = (const char *)((const T *)p.w + (u64)t.adapter * p.rank * p.in);
+    u32 xat[MR][4];
+#pragma unroll
+    for (int u = 0; u < 4; u++)
+#pragma unroll
+        for (int i = 0; i < MR; i++) xat[i][u] = min(i * 16 + slab_row(lane, u), last) * (u32)p.ldx * (u32)sizeof(T) + slab_byte(lane);
+    f32x4 acc[MR][NR];
+#pragma unroll
+    for (int i = 0; i < MR; i++)
+#pragma unroll
+        for (int j = 0; j < NR; j++) acc[i][j] = f32x4{ 0.f, 0.f, 0.f, 0.f };
+
+    // the sums over a slab: its weights in the LDS, x in registers
+    const auto multiply = [&](const Frag (&to)[CHUNKS], Frag (&a)[MR][4]) {
+        const int AHEAD = NR == 4;              // (the registers of the highest ranks do not hold a second one)
+        Frag b[AHEAD + 1][4];
+        const auto read = [&](int j) {
+#pragma unroll
+            for (int u = 0; u < 4; u++) b[j & AHEAD][u] = to[(j * 16 + m) * 16 + ((group * 4 + u) ^ m)];
+        };
+        if (AHEAD) read(0);
+#pragma unroll
+        for (int i = 0; i < MR; i++) quad_swap(a[i]);
+#pragma unroll
+        for (int j = 0; j < NR; j++) {
+            if (j + AHEAD < NR) read(j + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+#pragma unroll
+                for (int i = 0; i < MR; i++) acc[i][j] = mma(b[j & AHEAD][u], a[i][u], acc[i][j]);
+        }
+    };
+    // (chunk numbers mixed with the row's: 16 rows of one chunk lie in 16 places)
+    const auto place = [&](u32 k) { return (k * 16 + local / 16) * 16 + (local % 16 ^ local / 16); };
+    const u32 slabs = p.in / SLAB, shares = p.h.splits * 2, share = blockIdx.y * 2 + mine, trips = (slabs + shares - 1) / shares;
+    // Each half takes a run of slabs (55 us for 8192 x 16384 in 16 bits and rank 64, against 64 with slabs taken in turn), and
+    // tiles begin at different places.
+    const u32 turn = slabs ? blockIdx.x * 5 % slabs : 0;
+    u32 wat[FILL];
+#pragma unroll
+    for (int k = 0; k < FILL; k++) wat[k] = min(k * 16 + local / 16, p.rank - 1) * p.in * (u32)sizeof(T) + local % 16 * 16;
+    const auto fetch = [&](u32 trip, Frag (&fill)[FILL], Frag (&a)[MR][4]) {    // slab `trip` of this half's
+        const u32 s = share * trips + trip;
+        if (s < slabs) {
+            const u64 at = (u64)(s + turn < slabs ? s + turn : s + turn - slabs) * SLAB_BYTES;
+#pragma unroll
+            for (int k = 0; k < FILL; k++) fill[k] = load_some<EPL>((const T *)(w + at + wat[k]));
+#pragma unroll
+            for (int i = 0; i < MR; i++)
+#pragma unroll
+                for (int u = 0; u < 4; u++) a[i][u] = load_some<EPL>((const T *)(x + at + xat[i][u]));
+        } else {
+#pragma unroll
+            for (int k = 0; k < FILL; k++) fill[k] = Frag{};
+#pragma unroll
+            for (int i = 0; i < MR; i++)
+#pragma unroll
+                for (int u = 0; u < 4; u++) a[i][u] = Frag{};
+        }
+    };
+    // One trip: what was fetched goes to the LDS, the next is fetched, the sums are made.  A panel is written again in the
+    // trip after next, when all are past it.
+    const auto trip = [&](u32 k, Frag (&fill)[FILL], Frag (&a)[MR][4], Frag (&fill2)[FILL], Frag (&a2)[MR][4]) {
+        Frag(&to)[CHUNKS] = panel[k & 1][mine];
+#pragma unroll
+        for (int i = 0; i < FILL; i++) to[place(i)] = fill[i];
+        __syncthreads();
+        if (k + 1 < trips) fetch(k + 1, fill2, a2);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(to, a);
+    };
+    Frag fill[2][FILL], a[2][MR][4];
+    if (trips) fetch(0, fill[0], a[0]);
+    u32 k = 0;
+    for (; k + 2 <= trips; k += 2) {
+        trip(k, fill[0], a[0], fill[1], a[1]);
+        trip(k + 1, fill[1], a[1], fill[0], a[0]);
+    }
+    if (k < trips) trip(k, fill[0], a[0], fill[1], a[1]);
+    if (slabs * SLAB < p.in && blockIdx.y == p.h.splits - 1) {      // what is left of a row, by the last one's first half
+        const u64 at = (u64)slabs * SLAB_BYTES;
+        const int n = mine ? 0 : (int)(p.in - slabs * SLAB), nx = n - (int)(slab_byte(lane) / sizeof(T));
+#pragma unroll
+        for (int i = 0; i < FILL; i++) fill[0][i] = load_first<EPL>((const T *)(w + at + wat[i]), n - (int)(local % 16 * EPL));
+#pragma unroll
+        for (int i = 0; i < MR; i++)
+#pragma unroll
+            for (int u = 0; u < 4; u++) a[0][i][u] = load_first<EPL>((const T *)(x + at + xat[i][u]), nx);
+        Frag(&to)[CHUNKS] = panel[trips & 1][mine];
+#pragma unroll
+        for (int i = 0; i < FILL; i++) to[place(i)] = fill[0][i];
+        __syncthreads();
+        multiply(to, a[0]);
+    }
+
+    // the second half's sums to the first, through the LDS
+    const float scale = p.scales ? p.scales[t.adapter] : p.scale;
+    f32x4 *const part = (f32x4 *)panel;
+    __syncthreads();
+    if (mine == 1) {
+#pragma unroll
+        for (int i = 0; i < MR; i++)
+#pragma unroll
+            for (int j = 0; j < NR; j++) part[((wave & 3) * MR * NR + i * NR + j) * 64 + lane] = acc[i][j];
+    }
+    __syncthreads();
+    if (mine == 1) return;
+#pragma unroll
+    for (int i = 0; i < MR; i++)
+#pragma unroll
+        for (int j = 0; j < NR; j++) {
+            const f32x4 other = part[(wave * MR * NR + i * NR + j) * 64 + lane];
+            const u32 row = i * 16 + m, col = j * 16 + group * 4;
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[e] = col + e < p.rank ? (acc[i][j][e] + other[e]) * scale : 0.f;
+            if (row < rows) store_hidden<T>(p.h, v, t.row + first + row, col, blockIdx.y, p.q.rows);
+        }
 }
 
 // ---- up: out[row][c] = base[row][c] + sum_j hidden[row][j] w[c][j] ---------------------------------------------------
 
 struct UpParams {
-    const float *hidden;        // [splits][rows][padded]
+    Hidden h;
     const void *w, *base;       // w [adapters][out][rank]; base nullable
     void *out;
     Requests q;
     u64 ldb, ldo;
-    u32 cols, rank, padded, splits, trips;
+    u32 cols, rank, trips, panels;
 };
 
-// MR x 16 rows; a wavefront makes 128 bytes of each row at a time, the four of them neighbours, `trips` times.
-template <class T, int MR, int JS>
+// Place of chunk `ch` (16 bytes along the rank) of column n of a panel, CPR chunks a column.  What 16 lanes read together
+// are columns of four quarters of the panel, four neighbours of each: those bits of n are mixed into the chunk's number so
+// that they lie in 16 places of 16 bytes that the LDS has at once.
+template <int CPR, int QUARTER>
+DI u32 panel_place(u32 n, u32 ch)
+{
+    const u32 q = n / QUARTER & 3;
+    const u32 f = CPR == 4 ? q : CPR == 8 ? (n >> 1 & 1) | q << 1 : (n & 3) | q << 2;
+    return n * CPR + (ch ^ f);
+}
+
+// Tiles of WR x MR x 16 rows.  A wavefront makes 256 bytes of each of its MR x 16 rows at a time, `trips` times.  WR = 4:
+// the four of them have rows of their own and the same columns, whose part of w they share; WR = 1: the same rows, and
+// columns and panels of their own.
+template <class T, int MR, int JS, int WR>
 __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
 {
     typedef typename Mma<T>::Frag Frag;
-    const int EPL = Mma<T>::EPL, STEP = Mma<T>::STEP, WIDE = 128 / sizeof(T), QN = EPL / 4;
+    const int EPL = Mma<T>::EPL, STEP = Mma<T>::STEP, QN = EPL / 4, SLAB = SLAB_BYTES / sizeof(T), CPR = JS * STEP / EPL;
+    const int PANELS = 4 / WR, FILL = SLAB * CPR / (64 * WR);       // chunks of a panel that a lane fetches
+    __shared__ Frag panel[WR == 4 ? 2 : 1][PANELS][SLAB * CPR];
     Tile t;
-    if (!find_tile<MR * 16>(p.q, blockIdx.x, &t)) return;
-    const u32 lane = lane_id(), m = lane & 15, group = lane >> 4;
-    u32 col = (blockIdx.y * p.trips * 4 + wave_of_group()) * WIDE;
-    T *const out = (T *)p.out + (u64)t.row * p.ldo;
-    const T *const base = p.base ? (const T *)p.base + (u64)t.row * p.ldb : nullptr;
+    const u32 block = die_order(blockIdx.x, gridDim.x);
+    if (!find_tile<WR * MR * 16>(p.q, block / p.panels, &t)) return;
+    const u32 lane = lane_id(), m = lane & 15, group = lane >> 4, wave = wave_of_group();
+    const u32 first = WR == 4 ? wave * MR * 16 : 0, rows = t.rows > first ? t.rows - first : 0, mine = WR == 4 ? 0 : wave;
+    u32 col = (block % p.panels * p.trips * PANELS + mine) * SLAB;
     if (t.adapter < 0) {
         if (p.base == p.out) return;
-        for (u32 trip = 0; trip < p.trips; trip++, col += 4 * WIDE)
-            for (u32 r = 0; r < t.rows; r++)
-                for (u32 c = col + lane; c < min(col + WIDE, p.cols); c += 64)
+        T *const out = (T *)p.out + (u64)(t.row + first) * p.ldo;
+        const T *const base = p.base ? (const T *)p.base + (u64)(t.row + first) * p.ldb : nullptr;
+        for (u32 trip = 0; trip < p.trips; trip++, col += PANELS * SLAB)
+            for (u32 r = 0; r < min(rows, (u32)MR * 16); r++)
+                for (u32 c = col + lane; c < min(col + SLAB, p.cols); c += 64)
                     out[r * p.ldo + c] = base ? base[r * p.ldb + c] : (T)0.f;
         return;
     }
-    // hidden, rounded to the type of the tensors: half a step of the type for each term of the sum over the rank
+    const u32 last = rows ? rows - 1 : 0;
+    const u64 row0 = t.row + (rows ? first : 0);    // rows beyond the tile are its last one again, and not stored
     Frag h[MR][JS];
 #pragma unroll
-    for (int i = 0; i < MR; i++)
+    for (int i = 0; i < MR; i++) {
+        const u64 row = row0 + min(i * 16 + m, last);
 #pragma unroll
         for (int s = 0; s < JS; s++) {
             const u32 j = s * STEP + group * EPL;
-            float v[EPL] = {};
-            if (j < p.padded) {
-                const float *from = p.hidden + (u64)(t.row + min(i * 16 + m, t.rows - 1)) * p.padded + j;
-                for (u32 u = 0; u < p.splits; u++, from += (u64)p.q.rows * p.padded)
+            if (j >= p.h.padded) {
+#pragma unroll
+                for (int e = 0; e < EPL; e++) h[i][s][e] = (T)0.f;
+            } else if (!p.h.parts) {
+                h[i][s] = *(const Frag *)((const T *)p.h.up + up_place<T>(row, j, p.h.padded));
+            } else {
+                float v[EPL] = {};
+                const float *from = p.h.parts + row * p.h.padded + j;
+                for (u32 u = 0; u < p.h.splits; u++, from += (u64)p.q.rows * p.h.padded)
 #pragma unroll
                     for (int e = 0; e < EPL; e += 4) {
                         const f32x4 f = *(const f32x4 *)(from + e);
 #pragma unroll
                         for (int k = 0; k < 4; k++) v[e + k] += f[k];
                     }
+#pragma unroll
+                for (int e = 0; e < EPL; e++) h[i][s][e] = (T)v[e];
             }
-#pragma unroll
-            for (int e = 0; e < EPL; e++) h[i][s][e] = (T)v[e];
         }
+    }
     const T *const w = (const T *)p.w + (u64)t.adapter * p.cols * p.rank;
-    for (u32 trip = 0; trip < p.trips; trip++, col += 4 * WIDE) {
+    const char *const base = p.base ? (const char *)((const T *)p.base + row0 * p.ldb) : nullptr;
+    char *const out = (char *)((T *)p.out + row0 * p.ldo);
+    u32 yat[MR][4];
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-            const u32 c0 = col + half * (WIDE / 2);
-            if (c0 >= p.cols) return;
-            // product q has the columns whose place in a lane's EPL is 4 q to 4 q + 3
-            Frag b[QN][JS];
+    for (int i = 0; i < MR; i++)
+#pragma unroll
+        for (int u = 0; u < 4; u++) yat[i][u] = min(i * 16 + slab_row(lane, u), last) * (u32)p.ldb * (u32)sizeof(T);
+    for (u32 trip = 0; trip < p.trips; trip++, col += PANELS * SLAB) {
+        Frag(&to)[SLAB * CPR] = panel[WR == 4 ? trip & 1 : 0][mine];
+        const u32 c = col + slab_byte(lane) / sizeof(T);
+        Frag y[MR][4], fill[FILL];
+        const bool whole = p.rank % EPL == 0 && col + SLAB <= p.cols;
+        if (LIKELY(whole)) {        // no chunk is cut: one that is beyond the rank is another one, cleared
+#pragma unroll
+            for (int k = 0; k < FILL; k++) {
+                const u32 at = k * 64 * WR + (WR == 4 ? threadIdx.x : lane), j = at % CPR * EPL;
+                fill[k] = load_some<EPL>(w + (u64)(col + at / CPR) * p.rank + min(j, p.rank - EPL));
+                if (j >= p.rank) fill[k] = Frag{};
+            }
+            if (base) {
+#pragma unroll
+                for (int i = 0; i < MR; i++)
+#pragma unroll
+                    for (int u = 0; u < 4; u++) y[i][u] = load_some<EPL>((const T *)(base + yat[i][u]) + c);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < FILL; k++) {
+                const u32 at = k * 64 * WR + (WR == 4 ? threadIdx.x : lane), n = min(col + at / CPR, p.cols - 1), j = at % CPR * EPL;
+                fill[k] = load_first<EPL>(w + (u64)n * p.rank + j, (int)p.rank - (int)j);
+            }
+            if (base) {
+#pragma unroll
+                for (int i = 0; i < MR; i++)
+#pragma unroll
+                    for (int u = 0; u < 4; u++) y[i][u] = load_first<EPL>((const T *)(base + yat[i][u]) + c, (int)p.cols - (int)c);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < FILL; k++) {
+            const u32 at = k * 64 * WR + (WR == 4 ? threadIdx.x : lane);
+            to[panel_place<CPR, SLAB / 4>(at / CPR, at % CPR)] = fill[k];
+        }
+        // shared: this panel is written again in the trip after next, when all are past it; a wavefront's own: the LDS
+        // answers it in order
+        if (WR == 4)
+            __syncthreads();
+        else
+            wave_sync();
+        if (!rows || col >= p.cols) continue;
+        if (base) {
+#pragma unroll
+            for (int i = 0; i < MR; i++) quad_swap(y[i]);
+        }
+        // Product (u, q) has the columns whose place in the slab is SLAB / 4 group + EPL u + 4 q + 0 to 3: a lane ends up
+        // with EPL consecutive columns of one row in its register u, as it has them of y.
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            f32x4 acc[MR][QN];
 #pragma unroll
             for (int q = 0; q < QN; q++) {
-                const u32 c = min(c0 + (m >> 2) * EPL + q * 4 + (m & 3), p.cols - 1);
+                const u32 n = (m >> 2) * (SLAB / 4) + u * EPL + q * 4 + (m & 3);
+#pragma unroll
+                for (int i = 0; i < MR; i++) acc[i][q] = f32x4{ 0.f, 0.f, 0.f, 0.f };
 #pragma unroll
                 for (int s = 0; s < JS; s++) {
-                    const u32 j = s * STEP + group * EPL;
-                    b[q][s] = load_first<EPL>(w + (u64)c * p.rank + j, (int)p.rank - (int)j);
+                    const Frag b = to[panel_place<CPR, SLAB / 4>(n, s * (STEP / EPL) + group)];
+#pragma unroll
+                    for (int i = 0; i < MR; i++) acc[i][q] = mma(b, h[i][s], acc[i][q]);
                 }
             }
-            const u32 c = c0 + group * EPL;
-            const int n = (int)p.cols - (int)c;
 #pragma unroll
-            for (int i = 0; i < MR; i++) {
-                const u32 row = i * 16 + m;
-                f32x4 acc[QN];
+            for (int i = 0; i < MR; i++)
 #pragma unroll
-                for (int q = 0; q < QN; q++) {
-                    acc[q] = f32x4{ 0.f, 0.f, 0.f, 0.f };
+                for (int e = 0; e < EPL; e++) y[i][u][e] = (T)((base ? (float)y[i][u][e] : 0.f) + acc[i][e >> 2][e & 3]);
+        }
+        const int n = (int)p.cols - (int)c;
 #pragma unroll
-                    for (int s = 0; s < JS; s++) acc[q] = mma(b[q][s], h[i][s], acc[q]);
-                }
-                if (row < t.rows && n > 0) {
-                    Frag y;
+        for (int i = 0; i < MR; i++) {
+            quad_swap(y[i]);
 #pragma unroll
-                    for (int e = 0; e < EPL; e++) y[e] = (T)0.f;
-                    if (base) y = load_first<EPL>(base + row * p.ldb + c, n);
+            for (int u = 0; u < 4; u++) {
+                const u32 row = i * 16 + slab_row(lane, u);
+                if (row >= rows) continue;
+                T *const dst = (T *)(out + row * (u32)p.ldo * (u32)sizeof(T)) + c;
+                if (LIKELY(n >= EPL)) {
+                    *reinterpret_cast<typename Some<T, EPL>::loose *>(dst) = y[i][u];
+                } else {
 #pragma unroll
-                    for (int e = 0; e < EPL; e++) y[e] = (T)((float)y[e] + acc[e >> 2][e & 3]);
-                    T *const to = out + row * p.ldo + c;
-                    if (LIKELY(n >= EPL)) {
-                        *reinterpret_cast<typename Some<T, EPL>::loose *>(to) = y;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < EPL; e++)
-                            if (e < n) to[e] = y[e];
-                    }
+                    for (int e = 0; e < EPL; e++)
+                        if (e < n) dst[e] = y[i][u][e];
                 }
             }
         }
@@ -309,33 +609,43 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
 
 // ---- outer: sums[chunk][adapter][j][c] = sum over the chunk's rows of hidden[row][j] v[row][c] ----------------------
 
-// The 16-bit kernels read hidden as operands of their type, eight rows a lane: [padded][stride].  The 32-bit one reads
-// [rows][padded].
+// whole hidden values from parts
 struct FoldParams {
-    const float *from[2];
-    void *to[2];
-    u32 splits[2];
-    u32 rows, padded, stride;
+    Hidden h[2];
+    bool up[2], outer[2];       // which of the layouts are wanted
+    u32 rows;
 };
 
 template <class T>
 __global__ __launch_bounds__(256) void lowrank_fold_kernel(const FoldParams p)
 {
-    const u32 job = blockIdx.z, j = blockIdx.y * 16 + (threadIdx.x & 15), row = (blockIdx.x * 16 + (threadIdx.x >> 4)) * 8;
-    if (!p.to[job]) return;
-    float v[8];
+    const Hidden &h = p.h[blockIdx.z];
+    const bool up = p.up[blockIdx.z], outer = p.outer[blockIdx.z];
+    const u32 quads = h.padded / 4;             // four values of four rows a lane
+    const u32 at = blockIdx.x * 256 + threadIdx.x, col = at % quads * 4, row = at / quads * 4;
+    if (row >= p.rows || !(up || outer)) return;
+    f32x4 v[4];
 #pragma unroll
-    for (int e = 0; e < 8; e++) v[e] = 0.f;
-    for (u32 u = 0; u < p.splits[job]; u++)
+    for (int r = 0; r < 4; r++) v[r] = f32x4{ 0.f, 0.f, 0.f, 0.f };
+    for (u32 u = 0; u < h.splits; u++)
 #pragma unroll
-        for (int e = 0; e < 8; e++)
-            if (row + e < p.rows) v[e] += p.from[job][((u64)u * p.rows + row + e) * p.padded + j];
-    if (sizeof(T) == 4) {
+        for (int r = 0; r < 4; r++)
+            if (row + r < p.rows) {
+                const f32x4 f = *(const f32x4 *)(h.parts + ((u64)u * p.rows + row + r) * h.padded + col);
 #pragma unroll
-        for (int e = 0; e < 8; e++)
-            if (row + e < p.rows) ((float *)p.to[job])[(u64)(row + e) * p.padded + j] = v[e];
-    } else if (row < p.stride) {
-        store8((T *)p.to[job] + (u64)j * p.stride + row, 8, v);
+                for (int e = 0; e < 4; e++) v[r][e] += f[e];
+            }
+    typedef typename Some<T, 4>::type Four;
+#pragma unroll
+    for (int r = 0; r < 4; r++) {
+        Four o, c;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            o[e] = (T)v[r][e];
+            c[e] = sizeof(T) == 4 ? (T)v[r][e] : (T)v[e][r];        // 16 bits: four rows of column col + r
+        }
+        if (up) *(Four *)((T *)h.up + up_place<T>(row + r, col, h.padded)) = o;
+        if (outer) *(Four *)((T *)h.outer + (sizeof(T) == 4 ? outer_place<T>(row + r, col, h.padded) : outer_place<T>(row, col + r, h.padded))) = c;
     }
 }
 
@@ -348,48 +658,57 @@ struct OuterJob {
 struct OuterParams {
     OuterJob job[2];
     Requests q;
-    u32 stride;
 };
 
 // two 16-bit elements of each of two registers, swapped: (a0 b0) and (a1 b1) of (a0 a1), (b0 b1)
 DI u32 low_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 DI u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// rows t .. t + 31 (n of them) of CQ columns a lane: acc[q][j] += v^T hidden
-template <class T, int CQ, int NR>
-DI void outer_step(const OuterJob &o, u32 stride, u32 t, u32 n, u32 col, int cols, f32x4 acc[CQ][NR])
+// Rows t to t + 31 of CQ columns a lane, and what belongs to them of hidden; 0 in the place of rows that are not from lo to
+// hi - 1, whatever lies there.  t is a multiple of 8.  WHOLE: all of these rows, and whole panels.
+template <class T, int CQ, int NR, bool WHOLE>
+DI void outer_load(const OuterJob &o, u32 t, u32 lo, u32 hi, u32 col, int cols, u32 (&v)[8][CQ / 2], typename Mma<T>::Frag (&h)[NR])
 {
     typedef typename Mma<T>::Frag Frag;
-    const u32 lane = lane_id(), m = lane & 15, group = lane >> 4;
-    u32 v[8][CQ / 2];
-    const T *const from = (const T *)o.v + col;
+    const u32 lane = lane_id(), m = lane & 15, r0 = t + (lane >> 4) * 8;
+    const T *const from = (const T *)o.v + r0 * o.ldv + col;
 #pragma unroll
     for (int e = 0; e < 8; e++) {
-        const u32 r = group * 8 + e;
-        typename Some<T, CQ>::type x;
-        if (LIKELY(r < n)) {
-            x = load_first<CQ>(from + (t + r) * o.ldv, cols);
-        } else {
-#pragma unroll
-            for (int q = 0; q < CQ; q++) x[q] = (T)0.f;
-        }
+        typename Some<T, CQ>::type x = {};
+        if (WHOLE)
+            x = load_some<CQ>(from + e * o.ldv);
+        else if (r0 + e >= lo && r0 + e < hi)
+            x = load_first<CQ>(from + e * o.ldv, cols);
         __builtin_memcpy(v[e], &x, sizeof x);
     }
-    Frag h[NR];
 #pragma unroll
-    for (int j = 0; j < NR; j++)
-        h[j] = load_first<8>((const T *)o.hidden + (u64)(j * 16 + m) * stride + t + group * 8, (int)n - (int)group * 8);
+    for (int j = 0; j < NR; j++) {
+        h[j] = Frag{};
+        if (WHOLE || (r0 + 8 > lo && r0 < hi)) h[j] = *(const Frag *)((const T *)o.hidden + outer_place<T>(r0, j * 16 + m, NR * 16));
+        if (!WHOLE) {
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (r0 + e < lo || r0 + e >= hi) h[j][e] = (T)0.f;
+        }
+    }
+}
+
+// acc[q][j] += v^T hidden for column q of a lane and the j-th 16 of the rank
+template <class T, int CQ, int NR>
+DI void outer_add(const u32 (&v)[8][CQ / 2], const typename Mma<T>::Frag (&h)[NR], f32x4 (&acc)[CQ][NR])
+{
+    typedef typename Mma<T>::Frag Frag;
 #pragma unroll
     for (int q = 0; q < CQ; q += 2) {
-        u32 lo[4], hi[4];
+        u32 low[4], high[4];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            lo[e] = low_halves(v[2 * e][q / 2], v[2 * e + 1][q / 2]);
-            hi[e] = high_halves(v[2 * e][q / 2], v[2 * e + 1][q / 2]);
+            low[e] = low_halves(v[2 * e][q / 2], v[2 * e + 1][q / 2]);
+            high[e] = high_halves(v[2 * e][q / 2], v[2 * e + 1][q / 2]);
         }
         Frag a, b;
-        __builtin_memcpy(&a, lo, sizeof a);
-        __builtin_memcpy(&b, hi, sizeof b);
+        __builtin_memcpy(&a, low, sizeof a);
+        __builtin_memcpy(&b, high, sizeof b);
 #pragma unroll
         for (int j = 0; j < NR; j++) {
             acc[q][j] = mma(a, h[j], acc[q][j]);
@@ -398,25 +717,28 @@ DI void outer_step(const OuterJob &o, u32 stride, u32 t, u32 n, u32 col, int col
     }
 }
 
-// the same in 32 bits, four rows an instruction
-template <int CQ, int NR>
-DI void outer_step32(const OuterJob &o, u32 t, u32 n, u32 col, int cols, f32x4 acc[CQ][NR])
+// the same in 32 bits, 16 rows, four an instruction
+template <int CQ, int NR, bool WHOLE>
+DI void outer_load32(const OuterJob &o, u32 t, u32 lo, u32 hi, u32 col, int cols, typename Some<float, CQ>::type (&v)[4], float (&h)[4][NR])
 {
     const u32 lane = lane_id(), m = lane & 15, group = lane >> 4;
-    typename Some<float, CQ>::type v[4];
-    float h[4][NR];
 #pragma unroll
     for (int e = 0; e < 4; e++) {
-        const u32 r = e * 4 + group;
-        if (LIKELY(r < n)) {
-            v[e] = load_first<CQ>((const float *)o.v + (t + r) * o.ldv + col, cols);
-        } else {
+        const u32 r = t + e * 4 + group;
+        const bool in = WHOLE || (r >= lo && r < hi);
+        v[e] = typename Some<float, CQ>::type{};
+        if (WHOLE)
+            v[e] = load_some<CQ>((const float *)o.v + r * o.ldv + col);
+        else if (in)
+            v[e] = load_first<CQ>((const float *)o.v + r * o.ldv + col, cols);
 #pragma unroll
-            for (int q = 0; q < CQ; q++) v[e][q] = 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < NR; j++) h[e][j] = r < n ? ((const float *)o.hidden)[(u64)(t + r) * (NR * 16) + j * 16 + m] : 0.f;
+        for (int j = 0; j < NR; j++) h[e][j] = in ? ((const float *)o.hidden)[outer_place<float>(r, j * 16 + m, NR * 16)] : 0.f;
     }
+}
+
+template <int CQ, int NR>
+DI void outer_add32(const typename Some<float, CQ>::type (&v)[4], const float (&h)[4][NR], f32x4 (&acc)[CQ][NR])
+{
 #pragma unroll
     for (int e = 0; e < 4; e++)
 #pragma unroll
@@ -438,6 +760,7 @@ __global__ __launch_bounds__(256) void lowrank_outer_kernel(const OuterParams p)
     const u32 lane = lane_id(), wave = wave_of_group();
     const u32 col = (panel * 16 + (lane & 15)) * CQ;
     const int cols = (int)o.cols - (int)col;
+    const bool panel_whole = (panel + 1) * 16 * CQ <= o.cols;
     const u32 from = chunk * o.chunk_rows, upto = min(from + o.chunk_rows, p.q.rows);
     f32x4 acc[CQ][NR];
 #pragma unroll
@@ -460,12 +783,26 @@ __global__ __launch_bounds__(256) void lowrank_outer_kernel(const OuterParams p)
         while (left) {
             const u32 at = first_lane(left);
             left &= left - 1;
-            const u32 end = from_lane(hi, at);
-            for (u32 t = from_lane(lo, at) + wave * STEP; t < end; t += 4 * STEP) {
-                if constexpr (sizeof(T) == 4)
-                    outer_step32<CQ, NR>(o, t, end - t, col, cols, acc);
-                else
-                    outer_step<T, CQ, NR>(o, p.stride, t, end - t, col, cols, acc);
+            const u32 begin = from_lane(lo, at), end = from_lane(hi, at);
+            for (u32 t = begin / 8 * 8 + wave * STEP; t < end; t += 4 * STEP) {
+                const bool whole = panel_whole && t >= begin && t + STEP <= end;
+                if constexpr (sizeof(T) == 4) {
+                    typename Some<float, CQ>::type v[4];
+                    float h[4][NR];
+                    if (LIKELY(whole))
+                        outer_load32<CQ, NR, true>(o, t, begin, end, col, cols, v, h);
+                    else
+                        outer_load32<CQ, NR, false>(o, t, begin, end, col, cols, v, h);
+                    outer_add32<CQ, NR>(v, h, acc);
+                } else {
+                    u32 v[8][CQ / 2];
+                    typename Mma<T>::Frag h[NR];
+                    if (LIKELY(whole))
+                        outer_load<T, CQ, NR, true>(o, t, begin, end, col, cols, v, h);
+                    else
+                        outer_load<T, CQ, NR, false>(o, t, begin, end, col, cols, v, h);
+                    outer_add<T, CQ, NR>(v, h, acc);
+                }
             }
         }
     }
@@ -559,33 +896,64 @@ __global__ __launch_bounds__(256) void lowrank_swap_kernel(const SwapParams p)
 
 u32 padded_rank(u32 rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
 
-// How a batch is cut.  A tile has as many rows as a request has on average, at most 64 (32 where the rank needs the
-// registers): larger tiles read the weights less often, smaller ones keep single tokens from paying for rows that are
-// not there.
+// Tiles of 16 * tile16 rows that a batch can have.
+u64 tiles_of(const vms_lowrank_args *a, u32 tile16)
+{
+    const u64 size = tile16 * 16, requests = a->n_requests;
+    const u64 tiles = a->d_starts ? a->rows / size + requests + 2 : (a->rows + size - 1) / size;
+    return tiles < a->rows ? tiles : a->rows;
+}
+
+const u32 DOWN_WAVES = 8;       // of a workgroup; twice that where the rank leaves the registers
+
+// Rows of a tile of `down`, in sixteens: no more than a request has on average, so that single tokens do not pay for rows that
+// are not there; at most four, two or one as the rank leaves registers; and fewer as long as there is not a tile for each
+// compute unit: larger tiles read the weights less often, but compute units without a tile read nothing.
+u32 tile_of(const vms_lowrank_args *a)
+{
+    const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
+    u32 t = each >= 48 ? 4 : each >= 24 ? 2 : 1;
+    t = a->rank > 64 ? 1 : a->rank > 32 && t > 2 ? 2 : t;
+    while (t > 1 && a->rows / (t * 16) < OPS_CUS) t /= 2;
+    return t;
+}
+
 struct Cut {
-    u32 tile16, tiles;      // 16 rows each; tiles there can be
+    u32 tile16, tiles, splits;  // tile16 8: the kernel with shared weights
 };
 
-Cut cut_of(const vms_lowrank_args *a)
+Cut cut_of(const vms_lowrank_args *a, u64 in)
 {
     Cut c;
     const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
-    c.tile16 = each >= 48 ? 4 : each >= 24 ? 2 : 1;
-    if (c.tile16 == 4 && padded_rank(a->rank) == 128) c.tile16 = 2;
-    const u64 size = c.tile16 * 16, tiles = a->d_starts ? a->rows / size + requests + 2 : (a->rows + size - 1) / size;
-    c.tiles = (u32)(tiles < a->rows ? tiles : a->rows);
-    if (!c.tiles) c.tiles = 1;
+    const bool shared = a->rank > 32 && each >= 128 && a->rows >= 2048;
+    c.tile16 = shared ? 8 : tile_of(a);
+    const u64 tiles = tiles_of(a, c.tile16), slabs = in * type_bytes(a->dtype) / SLAB_BYTES;
+    c.tiles = tiles ? (u32)tiles : 1;
+    // A workgroup for each compute unit, but a slab at least for a wavefront.  Where parts are put together before they are
+    // read it pays to fill all compute units; where `up` reads them, again for each of its panels, only if there are few.
+    const u64 most = slabs / (shared ? 2 : DOWN_WAVES);
+    u64 s = shared || c.tiles < OPS_CUS / 4 ? (OPS_CUS + c.tiles - 1) / c.tiles : 1;
+    if (s > most) s = most;
+    if (s > (shared ? 8 : 16)) s = shared ? 8 : 16;
+    c.splits = s ? (u32)s : 1;
     return c;
 }
 
-// workgroups that share the summed dimension: two on every compute unit, but two steps at least for a wavefront
-u32 splits_of(const vms_lowrank_args *a, const Cut &c, u64 in)
+size_t laid_out(const vms_lowrank_args *a) { return (a->rows + 15) / 16 * 16 * padded_rank(a->rank) * type_bytes(a->dtype); }
+
+size_t parts_bytes(const vms_lowrank_args *a, const Cut &c) { return c.splits > 1 ? (size_t)c.splits * a->rows * padded_rank(a->rank) * 4 : 0; }
+bool folded(const Cut &c) { return c.splits > 1 && c.tile16 == 8; }
+
+size_t hidden_bytes(const vms_lowrank_args *a, const Cut &c) { return (c.splits == 1 || folded(c) ? 2 * laid_out(a) : 0) + parts_bytes(a, c); }
+
+Hidden hidden_at(const vms_lowrank_args *a, const Cut &c, void *at)
 {
-    const u64 steps = in / (a->dtype == VMS_F32 ? 16 : 32), most = steps / 8;
-    u64 s = (2 * OPS_CUS + c.tiles - 1) / c.tiles;
-    if (s > most) s = most;
-    if (s > 16) s = 16;
-    return s ? (u32)s : 1;
+    const u32 padded = padded_rank(a->rank);
+    char *const p = (char *)at;
+    if (c.splits == 1) return Hidden{ p, p + laid_out(a), nullptr, 1, padded, false };
+    if (folded(c)) return Hidden{ p, p + laid_out(a), (float *)(p + 2 * laid_out(a)), c.splits, padded, true };
+    return Hidden{ nullptr, nullptr, (float *)p, c.splits, padded, false };
 }
 
 int check(const vms_lowrank_args *a)
@@ -598,10 +966,13 @@ int check(const vms_lowrank_args *a)
     return VMS_OK;
 }
 
+// places inside a tile of 128 rows are counted in 32 bits
+bool near_ok(u64 ld) { return ld < 1u << 23; }
+
 int check_inputs(const vms_lowrank_args *a)
 {
     if (!input_ok(a->d_a, a->dtype) || !input_ok(a->d_b, a->dtype)) return VMS_EINVAL;
-    if (a->rows && (!input_ok(a->d_x, a->dtype) || !stride_ok(a->ldx))) return VMS_EINVAL;
+    if (a->rows && (!input_ok(a->d_x, a->dtype) || !near_ok(a->ldx))) return VMS_EINVAL;
     if ((uintptr_t)a->d_scales % 4 || (uintptr_t)a->d_starts % 4 || (uintptr_t)a->d_which % 4) return VMS_EINVAL;
     if (a->d_starts && a->n_requests && !a->d_which) return VMS_EINVAL;
     if (a->rows && (!a->d_hidden || (uintptr_t)a->d_hidden % 16 || a->hidden_bytes < vms_lowrank_hidden_bytes(a))) return VMS_EWORKSPACE;
@@ -616,54 +987,74 @@ Requests requests_of(const vms_lowrank_args *a)
 template <class T, int MR>
 int launch_down(const DownParams &p, u32 tiles, void *stream)
 {
-    const dim3 grid(tiles, p.splits), block(256);
-    switch (padded_rank(p.rank)) {
-    case 16: return ops_launch(lowrank_down_kernel<T, MR, 1>, grid, block, 0, p, stream);
-    case 32: return ops_launch(lowrank_down_kernel<T, MR, 2>, grid, block, 0, p, stream);
-    case 64: return ops_launch(lowrank_down_kernel<T, MR, 4>, grid, block, 0, p, stream);
+    const dim3 grid(tiles, p.h.splits), block(DOWN_WAVES * 64), twice(DOWN_WAVES * 128);
+    switch (p.h.padded) {
+    case 16: return MR == 4 ? ops_launch(lowrank_down_kernel<T, 4, 1, DOWN_WAVES>, grid, block, 0, p, stream)
+                            : ops_launch(lowrank_down_kernel<T, MR == 4 ? 2 : MR, 1, DOWN_WAVES * 2>, grid, twice, 0, p, stream);
+    case 32: return MR == 4 ? ops_launch(lowrank_down_kernel<T, 4, 2, DOWN_WAVES>, grid, block, 0, p, stream)
+                            : ops_launch(lowrank_down_kernel<T, MR == 4 ? 2 : MR, 2, DOWN_WAVES * 2>, grid, twice, 0, p, stream);
+    case 64: return ops_launch(lowrank_down_kernel<T, MR == 4 ? 2 : MR, 4, DOWN_WAVES>, grid, block, 0, p, stream);
     }
-    return ops_launch(lowrank_down_kernel<T, MR == 4 ? 2 : MR, 8>, grid, block, 0, p, stream);
+    return ops_launch(lowrank_down_kernel<T, 1, 8, DOWN_WAVES>, grid, block, 0, p, stream);
 }
 
 template <class T>
-int down(const vms_lowrank_args *a, const Cut &c, const void *x, u64 ldx, const void *w, u64 in, float *hidden, void *stream)
+int fold(const FoldParams &p, void *stream)
 {
-    const DownParams p = { x, w, hidden, a->d_scales, requests_of(a), ldx, a->scale, (u32)in, a->rank, splits_of(a, c, in) };
+    const u32 lanes = (p.rows + 3) / 4 * (p.h[0].padded / 4);
+    return ops_launch(lowrank_fold_kernel<T>, dim3((lanes + 255) / 256, 1, 2), dim3(256), 0, p, stream);
+}
+
+// The hidden values, whole or in parts that `up` reads; in the order that the products over `in` leave them.
+template <class T>
+int down(const vms_lowrank_args *a, const Cut &c, const void *x, u64 ldx, const void *w, u64 in, Hidden *h, void *stream)
+{
+    const DownParams p = { x, w, *h, a->d_scales, requests_of(a), ldx, a->scale, (u32)in, a->rank };
+    const dim3 grid(c.tiles, c.splits), block(512);
+    int rc;
     switch (c.tile16) {
     case 1: return launch_down<T, 1>(p, c.tiles, stream);
     case 2: return launch_down<T, 2>(p, c.tiles, stream);
+    case 4: return launch_down<T, 4>(p, c.tiles, stream);
     }
-    return launch_down<T, 4>(p, c.tiles, stream);
+    rc = h->padded == 64 ? ops_launch(lowrank_down_shared_kernel<T, 4>, grid, block, 0, p, stream)
+                         : ops_launch(lowrank_down_shared_kernel<T, 8>, grid, block, 0, p, stream);
+    if (rc || !h->folded) return rc;
+    const FoldParams f = { { *h, *h }, { true, false }, { true, false }, (u32)a->rows };
+    rc = fold<T>(f, stream);
+    h->parts = nullptr;
+    return rc;
 }
 
-template <class T, int MR>
-int launch_up(const UpParams &p, dim3 grid, void *stream)
+template <class T, int MR, int WR>
+int launch_up(const UpParams &p, u32 grid, void *stream)
 {
     const dim3 block(256);
     const int per = Mma<T>::STEP;
-    switch (p.padded) {
-    case 16: return ops_launch(lowrank_up_kernel<T, MR, 1>, grid, block, 0, p, stream);
-    case 32: return ops_launch(lowrank_up_kernel<T, MR, 32 / per>, grid, block, 0, p, stream);
-    case 64: return ops_launch(lowrank_up_kernel<T, MR, 64 / per>, grid, block, 0, p, stream);
+    switch (p.h.padded) {
+    case 16: return ops_launch(lowrank_up_kernel<T, MR, 1, WR>, dim3(grid), block, 0, p, stream);
+    case 32: return ops_launch(lowrank_up_kernel<T, MR, 32 / per, WR>, dim3(grid), block, 0, p, stream);
+    case 64: return ops_launch(lowrank_up_kernel<T, MR, 64 / per, WR>, dim3(grid), block, 0, p, stream);
     }
-    return ops_launch(lowrank_up_kernel<T, MR == 4 ? 2 : MR, 128 / per>, grid, block, 0, p, stream);
+    return ops_launch(lowrank_up_kernel<T, MR, 128 / per, WR>, dim3(grid), block, 0, p, stream);
 }
 
 template <class T>
-int up(const vms_lowrank_args *a, const Cut &c, const float *hidden, u32 splits, const void *w, const void *base, u64 ldb, void *out,
-       u64 ldo, u64 cols, void *stream)
+int up(const vms_lowrank_args *a, const Hidden &h, const void *w, const void *base, u64 ldb, void *out, u64 ldo, u64 cols, void *stream)
 {
-    const u64 trip = 4 * 128 / sizeof(T), all = (cols + trip - 1) / trip;
-    // workgroups enough for eight on every compute unit before one takes a second trip
-    u64 trips = all * c.tiles / (OPS_CUS * 8);
+    const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
+    const u32 tile16 = each >= 512 ? 8 : each >= 48 ? 4 : 1, tiles = (u32)tiles_of(a, tile16);
+    const u64 trip = (tile16 == 1 ? 4 : 1) * SLAB_BYTES / sizeof(T), all = (cols + trip - 1) / trip;
+    // workgroups enough for four on every compute unit before one takes a second trip
+    u64 trips = all * tiles / (OPS_CUS * 4);
     trips = trips < 1 ? 1 : trips > 8 ? 8 : trips;
-    const UpParams p = { hidden, w, base, out, requests_of(a), ldb, ldo, (u32)cols, a->rank, padded_rank(a->rank), splits, (u32)trips };
-    const dim3 grid(c.tiles, (u32)((all + trips - 1) / trips));
-    switch (c.tile16) {
-    case 1: return launch_up<T, 1>(p, grid, stream);
-    case 2: return launch_up<T, 2>(p, grid, stream);
+    const UpParams p = { h, w, base, out, requests_of(a), ldb, ldo, (u32)cols, a->rank, (u32)trips, (u32)((all + trips - 1) / trips) };
+    const u32 grid = tiles * p.panels;
+    switch (tile16) {
+    case 1: return launch_up<T, 1, 1>(p, grid, stream);
+    case 4: return launch_up<T, 1, 4>(p, grid, stream);
     }
-    return launch_up<T, 4>(p, grid, stream);
+    return launch_up<T, 2, 4>(p, grid, stream);
 }
 
 // columns that a lane takes in the outer products: as many as the registers hold beside the rank
@@ -699,7 +1090,7 @@ int launch_outer(const OuterParams &p, u32 padded, dim3 grid, void *stream)
 struct Layout {
     size_t at, bt, dhidden, hfold, dfold, dasums, dbsums, total;
     OuterJob da, db;
-    u32 stride;
+    Cut forward, back;          // of the products over `in` and over `out`
 };
 
 bool wants_hidden_gradient(const vms_lowrank_backward_args *a) { return a->d_dx || a->d_da; }
@@ -708,20 +1099,19 @@ Layout layout_of(const vms_lowrank_backward_args *a)
 {
     const vms_lowrank_args &f = a->f;
     const size_t e = type_bytes(f.dtype), padded = padded_rank(f.rank);
-    const Cut c = cut_of(&f);
     Layout l = {};
     size_t end = 0;
     const auto place = [&end](size_t *at, size_t bytes) {
         *at = end;
         end += (bytes + 255) & ~(size_t)255;
     };
-    l.stride = (u32)((f.rows + 7) / 8 * 8);
-    const size_t folded = padded * l.stride * e;
+    l.forward = cut_of(&f, f.in);
+    l.back = cut_of(&f, f.out);
     place(&l.at, a->d_dx ? (size_t)f.n_adapters * f.rank * f.in * e : 0);
     place(&l.bt, wants_hidden_gradient(a) ? (size_t)f.n_adapters * f.rank * f.out * e : 0);
-    place(&l.dhidden, wants_hidden_gradient(a) ? (size_t)splits_of(&f, c, f.out) * f.rows * padded * 4 : 0);
-    place(&l.hfold, a->d_db ? folded : 0);
-    place(&l.dfold, a->d_da ? folded : 0);
+    place(&l.dhidden, wants_hidden_gradient(a) ? hidden_bytes(&f, l.back) : 0);
+    place(&l.hfold, a->d_db && l.forward.splits > 1 ? laid_out(&f) : 0);
+    place(&l.dfold, a->d_da && l.back.splits > 1 ? laid_out(&f) : 0);
     outer_cut(&f, f.in, &l.da);
     outer_cut(&f, f.out, &l.db);
     place(&l.dasums, a->d_da ? (size_t)l.da.chunks * f.n_adapters * padded * f.in * 4 : 0);
@@ -735,34 +1125,35 @@ int backward(const vms_lowrank_backward_args *a, void *stream)
 {
     const vms_lowrank_args &f = a->f;
     const u32 padded = padded_rank(f.rank);
-    const Cut c = cut_of(&f);
-    Layout l = layout_of(a);
+    const Layout l = layout_of(a);
     char *const ws = (char *)a->d_workspace;
-    float *const dhidden = (float *)(ws + l.dhidden);
+    Hidden h = hidden_at(&f, l.forward, f.d_hidden), dh = hidden_at(&f, l.back, ws + l.dhidden);
+    if (h.folded) h.parts = nullptr;            // the forward pass has put them together
     int rc = VMS_OK;
     if (wants_hidden_gradient(a)) {
         const auto blocks = [](u64 r, u64 k) { return (u32)((r + 31) / 32 * ((k + 31) / 32)); };
         SwapParams s = { { { f.d_b, ws + l.bt, (u32)f.out, f.rank, blocks(f.out, f.rank) }, { f.d_a, ws + l.at, f.rank, (u32)f.in, 0 } } };
         if (a->d_dx) s.job[1].blocks = blocks(f.rank, f.in);
         rc = ops_launch(lowrank_swap_kernel<T>, dim3(s.job[0].blocks + s.job[1].blocks, f.n_adapters), dim3(256), 0, s, stream);
-        if (!rc) rc = down<T>(&f, c, a->d_dout, a->lddout, ws + l.bt, f.out, dhidden, stream);
+        if (!rc) rc = down<T>(&f, l.back, a->d_dout, a->lddout, ws + l.bt, f.out, &dh, stream);
     }
-    if (!rc && a->d_dx) rc = up<T>(&f, c, dhidden, splits_of(&f, c, f.out), ws + l.at, nullptr, 0, a->d_dx, a->lddx, f.in, stream);
+    if (!rc && a->d_dx) rc = up<T>(&f, dh, ws + l.at, nullptr, 0, a->d_dx, a->lddx, f.in, stream);
     if (rc || !(a->d_da || a->d_db)) return rc;
-    const FoldParams fold = { { f.d_hidden, dhidden },
-                              { a->d_db ? ws + l.hfold : nullptr, a->d_da ? ws + l.dfold : nullptr },
-                              { splits_of(&f, c, f.in), splits_of(&f, c, f.out) },
-                              (u32)f.rows, padded, l.stride };
-    rc = ops_launch(lowrank_fold_kernel<T>, dim3((u32)((f.rows + 127) / 128), padded / 16, 2), dim3(256), 0, fold, stream);
-    if (rc) return rc;
-    OuterParams o = { { l.da, l.db }, requests_of(&f), l.stride };
+    FoldParams some = { { h, dh }, {}, { a->d_db && h.parts, a->d_da && dh.parts }, (u32)f.rows };
+    if (some.outer[0]) h.outer = some.h[0].outer = ws + l.hfold;
+    if (some.outer[1]) dh.outer = some.h[1].outer = ws + l.dfold;
+    if (some.outer[0] || some.outer[1]) {
+        rc = fold<T>(some, stream);
+        if (rc) return rc;
+    }
+    OuterParams o = { { l.da, l.db }, requests_of(&f) };
     o.job[0].v = f.d_x;
     o.job[0].ldv = f.ldx;
-    o.job[0].hidden = ws + l.dfold;
+    o.job[0].hidden = dh.outer;
     o.job[0].sums = (float *)(ws + l.dasums);
     o.job[1].v = a->d_dout;
     o.job[1].ldv = a->lddout;
-    o.job[1].hidden = ws + l.hfold;
+    o.job[1].hidden = h.outer;
     o.job[1].sums = (float *)(ws + l.dbsums);
     JoinParams j = { { { o.job[0].sums, a->d_da, (u32)f.in, l.da.chunks, 0 }, { o.job[1].sums, a->d_db, (u32)f.out, l.db.chunks, 1 } },
                      f.rank, padded, (u32)((f.in + 255) / 256) };
@@ -791,7 +1182,7 @@ __global__ __launch_bounds__(256) void lowrank_clear_kernel(const ClearParams p)
 extern "C" size_t vms_lowrank_hidden_bytes(const vms_lowrank_args *a)
 {
     if (check(a)) return 0;
-    return (size_t)splits_of(a, cut_of(a), a->in) * a->rows * padded_rank(a->rank) * sizeof(float);
+    return hidden_bytes(a, cut_of(a, a->in));
 }
 
 extern "C" int vms_lowrank(const vms_lowrank_args *a, void *stream)
@@ -801,13 +1192,14 @@ extern "C" int vms_lowrank(const vms_lowrank_args *a, void *stream)
     if (!a->rows) return VMS_OK;
     rc = check_inputs(a);
     if (rc) return rc;
-    if (!input_ok(a->d_y, a->dtype) || !stride_ok(a->ldy) || !output_ok(a->d_out, a->dtype, a->ldo, a->out) || !stride_ok(a->ldo)) return VMS_EINVAL;
+    if (!input_ok(a->d_y, a->dtype) || !near_ok(a->ldy) || !output_ok(a->d_out, a->dtype, a->ldo, a->out) || !near_ok(a->ldo)) return VMS_EINVAL;
     if (a->d_y == a->d_out && a->ldy != a->ldo) return VMS_EINVAL;
-    const Cut c = cut_of(a);
+    const Cut c = cut_of(a, a->in);
+    Hidden h = hidden_at(a, c, a->d_hidden);
     return with_type(a->dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        const int r = down<T>(a, c, a->d_x, a->ldx, a->d_a, a->in, a->d_hidden, stream);
-        return r ? r : up<T>(a, c, a->d_hidden, splits_of(a, c, a->in), a->d_b, a->d_y, a->ldy, a->d_out, a->ldo, a->out, stream);
+        const int r = down<T>(a, c, a->d_x, a->ldx, a->d_a, a->in, &h, stream);
+        return r ? r : up<T>(a, h, a->d_b, a->d_y, a->ldy, a->d_out, a->ldo, a->out, stream);
     });
 }
 
@@ -834,8 +1226,8 @@ extern "C" int vms_lowrank_backward(const vms_lowrank_backward_args *a, void *st
     }
     rc = check_inputs(&f);
     if (rc) return rc;
-    if (!input_ok(a->d_dout, f.dtype) || !stride_ok(a->lddout)) return VMS_EINVAL;
-    if (a->d_dx && (!output_ok(a->d_dx, f.dtype, a->lddx, f.in) || !stride_ok(a->lddx))) return VMS_EINVAL;
+    if (!input_ok(a->d_dout, f.dtype) || !near_ok(a->lddout)) return VMS_EINVAL;
+    if (a->d_dx && (!output_ok(a->d_dx, f.dtype, a->lddx, f.in) || !near_ok(a->lddx))) return VMS_EINVAL;
     if (!a->d_dx && !a->d_da && !a->d_db) return VMS_OK;
     if (!a->d_workspace || (uintptr_t)a->d_workspace % 16 || a->workspace_bytes < layout_of(a).total) return VMS_EWORKSPACE;
     return with_type(f.dtype, [&](auto *t) { return backward<std::remove_pointer_t<decltype(t)>>(a, stream); });

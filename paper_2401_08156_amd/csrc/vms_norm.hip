@@ -435,22 +435,33 @@ __global__ __launch_bounds__(1024) void norm_back_long_kernel(const NormBackPara
     }
 }
 
-// dweight and dbias from the workgroups' sums: 32 columns a workgroup, its eight rows of lanes take every eighth part
+// dweight and dbias from the workgroups' sums: 32 columns a workgroup, its 32 rows of lanes take every 32nd part
 template <class T>
-__global__ __launch_bounds__(256) void norm_join_kernel(const NormJoinParams p)
+__global__ __launch_bounds__(1024) void norm_join_kernel(const NormJoinParams p)
 {
-    __shared__ float sums[8][33];
+    __shared__ float sums[32][33];
     const u32 x = threadIdx.x & 31, y = threadIdx.x >> 5, k = blockIdx.y;
     T *const out = (T *)(k ? p.dbias : p.dweight);
+    if (!out) return;
     const u32 col = blockIdx.x * 32 + x;
     float v = 0.f;
-    if (out && col < p.cols)
-        for (u32 i = y; i < p.parts; i += 8) v += p.partial[((u64)i * 2 + k) * p.cols + col];
+    if (col < p.cols) {
+        const float *from = p.partial + k * (u64)p.cols + col;
+        const u64 apart = 2 * (u64)p.cols;
+        u32 i = y;
+        for (; i + 96 < p.parts; i += 128) {
+            float f[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++) f[u] = from[(i + 32 * u) * apart];
+            v += (f[0] + f[1]) + (f[2] + f[3]);
+        }
+        for (; i < p.parts; i += 32) v += from[i * apart];
+    }
     sums[y][x] = v;
     __syncthreads();
-    if (y == 0 && out && col < p.cols) {
+    if (y == 0 && col < p.cols) {
 #pragma unroll
-        for (int i = 1; i < 8; i++) v += sums[i][x];
+        for (int i = 1; i < 32; i++) v += sums[i][x];
         out[col] = (T)v;
     }
 }
@@ -580,6 +591,6 @@ extern "C" int vms_layernorm_backward(const vms_layernorm_backward_args *a, void
         }
         if (!weights) return (int)VMS_OK;
         const NormJoinParams j = { (const float *)a->d_workspace, a->d_dweight, a->d_dbias, grid, p.cols };
-        return ops_launch(norm_join_kernel<T>, dim3((p.cols + 31) / 32, 2), dim3(256), 0, j, stream);
+        return ops_launch(norm_join_kernel<T>, dim3((p.cols + 31) / 32, 2), dim3(1024), 0, j, stream);
     });
 }

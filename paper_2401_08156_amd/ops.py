@@ -318,7 +318,7 @@ def _low_rank(y, x, a, b, scale, starts, which, inplace):
     else:
         out, f.ldo = torch.empty(y.shape, dtype=y.dtype, device=y.device), y.size(-1)
     f.hidden_bytes = (_lib or lib()).vms_lowrank_hidden_bytes(ctypes.addressof(f))
-    hidden = torch.empty(f.hidden_bytes // 4, dtype=torch.float32, device=x.device)
+    hidden = torch.empty(f.hidden_bytes, dtype=torch.uint8, device=x.device)
     f.d_hidden, f.d_y, f.d_out, f.ldy = hidden.data_ptr(), base.data_ptr(), out.data_ptr(), ldy
     _call("vms_lowrank", f, x.device)
     return out, hidden
@@ -345,7 +345,7 @@ class _LowRankAdd(torch.autograd.Function):
         m, ldx = _matrix(x)
         d, ldd = _matrix(dout)
         f = _low_rank_args(m, ldx, _rows(x)[0], a, b, ctx.scale if scales is None else scales, starts, which)
-        f.d_hidden, f.hidden_bytes = hidden.data_ptr(), hidden.numel() * 4
+        f.d_hidden, f.hidden_bytes = hidden.data_ptr(), hidden.numel()
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
         da = torch.empty_like(a) if need_a else None
         db = torch.empty_like(b) if need_b else None
@@ -368,7 +368,7 @@ def low_rank_add(y, x, a, b, scale=1.0, starts=None, which=None, inplace=False):
     tensor with one for each adapter.  Ranks up to 128.
 
     `inplace` makes the sum in y itself and leaves rows of no request untouched.  Gradients: of y, x, a and b; an
-    adapter's are summed over all its requests.  Kept for the backward pass: x, a, b, and 4 to 64 bytes for each row and rank."""
+    adapter's are summed over all its requests.  Kept for the backward pass: x, a, b, and scale * x a^T."""
     _same(x, y=y, a=a, b=b)
     if x.dim() == 0 or x.shape[:-1] != y.shape[:-1]:
         raise ValueError("x has shape %s, y %s" % (tuple(x.shape), tuple(y.shape)))

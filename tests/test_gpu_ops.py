@@ -306,6 +306,14 @@ def test_long_batches(dtype):
     check_low_rank(2100, 256, 384, 64, dtype, 2, [0, 1000, 1003, 2090], [1, 0, 1])
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rank", [40, 64, 128])
+def test_long_requests_of_high_rank(rank, dtype):
+    # sums shared by workgroups and put together again, odd lengths of rows and of the last slab
+    check_low_rank(2055, 1600, 900, rank, dtype, 2, [5, 900, 1003, 2049], [1, 0, 1])
+    check_low_rank(2048, 1111, 1300, rank, dtype, flat=True)
+
+
 def test_single_tokens_through_wide_layers():
     for rank in (1, 16, 64):
         check_low_rank(1, 8192, 8192, rank, torch.bfloat16, step=False, flat=True)
