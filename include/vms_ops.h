@@ -116,9 +116,8 @@ int vms_layernorm_backward(const vms_layernorm_backward_args *a, void *stream);
  * d_y = d_out (same stride): the sum is made in place, and rows of no request are not touched.
  *
  * d_hidden (vms_lowrank_hidden_bytes, 16-byte aligned) receives scale * x a^T: workspace of the forward
- * pass, and what the backward pass reads.  In a layout of the library's own, rounded to the type (a
- * value that float16 does not hold becomes an infinity there, as it does in a program that stores it),
- * or as sums in parts.                                                                            */
+ * pass, and what the backward pass reads, in a layout of the library's own with 16 bits or more of each
+ * value (one that float16 does not hold is an infinity there, as in a program that stores it).    */
 #define VMS_LOWRANK_MAX_RANK 128
 typedef struct vms_lowrank_args {
     uint32_t struct_size;        /* sizeof(vms_lowrank_args)                                        */

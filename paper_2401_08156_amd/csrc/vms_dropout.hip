@@ -14,7 +14,7 @@ struct DropoutParams {
 
 // A lane takes groups of eight consecutive elements of a row, `step` groups apart.  Their row and place in it are found by
 // one division and carried on by additions.
-template <class T>
+template <class T, bool ONCE>
 __global__ __launch_bounds__(256) void dropout_kernel(const DropoutParams p)
 {
     const u64 seed = p.mask.limit ? mask_seed(p.mask) : 0;
@@ -25,15 +25,15 @@ __global__ __launch_bounds__(256) void dropout_kernel(const DropoutParams p)
     for (; at < p.groups; at += step) {
         const u32 col = group * 8, n = p.cols - col;
         float v[8];
-        load8((const T *)p.x + row * p.ldx + col, n, v);
+        load8<ONCE>((const T *)p.x + row * p.ldx + col, n, v);
         float r[8];
-        if (p.residual) load8((const T *)p.residual + row * p.ldr + col, n, r);
+        if (p.residual) load8<ONCE>((const T *)p.residual + row * p.ldr + col, n, r);
         if (p.mask.limit) drop8(p.mask, seed, row, group, v);
         if (p.residual) {
 #pragma unroll
             for (int i = 0; i < 8; i++) v[i] += r[i];
         }
-        store8((T *)p.y + row * p.ldy + col, n, v);
+        store8<ONCE>((T *)p.y + row * p.ldy + col, n, v);
         row += step_rows;
         group += step_groups;
         if (group >= p.per_row) {
@@ -68,9 +68,10 @@ extern "C" int vms_dropout(const vms_dropout_args *a, void *stream)
     p.per_row = (p.cols + 7) / 8;
     p.groups = (u64)p.rows * p.per_row;
     const u64 blocks = (p.groups + 255) / 256;
-    const u32 grid = (u32)(blocks < OPS_CUS * 8 ? blocks : OPS_CUS * 8);
+    const u32 grid = (u32)(blocks < OPS_CUS * 32 ? blocks : OPS_CUS * 32);
+    const bool once = passes_by(a->rows * a->cols * type_bytes(a->dtype) * (a->d_residual ? 3 : 2));
     return with_type(a->dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        return ops_launch(dropout_kernel<T>, dim3(grid), dim3(256), 0, p, stream);
+        return ops_launch(once ? dropout_kernel<T, true> : dropout_kernel<T, false>, dim3(grid), dim3(256), 0, p, stream);
     });
 }

@@ -22,12 +22,12 @@ namespace {
 // at EPL * group; 4 EPL elements are a step.  Result: column m, rows 4 group to 4 group + 3.
 template <class T>
 struct Mma {
-    static const int EPL = 8, STEP = 32;
+    static const int EPL = 8, STEP = 32, PLANES = 2;
     typedef T Frag __attribute__((ext_vector_type(8)));
 };
 template <>
 struct Mma<float> {
-    static const int EPL = 4, STEP = 16;
+    static const int EPL = 4, STEP = 16, PLANES = 1;
     typedef f32x4 Frag;
 };
 DI f32x4 mma(Mma<float>::Frag a, Mma<float>::Frag b, f32x4 c)
@@ -147,15 +147,19 @@ DI bool find_tile(const Requests &q, u32 tile, Tile *out)
 
 // ---- down: hidden[row][j] = scale sum_k x[row][k] w[j][k] ------------------------------------------------------------
 
-// What a batch's hidden values are kept as.  Whole sums are rounded to the type of the tensors, as the products that read
-// them take them: half a step of the type for each term of a sum over the rank.  They are laid out twice, in the order in
-// which the lanes of `up` and of `outer` read them, padded to 16 rows.  Where there are not tiles enough for the compute
-// units, workgroups share the summed dimension and leave parts of the sums, in 32 bits: [splits][rows][padded].
+// What a batch's hidden values are kept as.  They are sums, and the products that read them take the type of the tensors.  In
+// 16 bits a value of a small batch goes through as two, itself rounded and what that left, in two planes; that costs
+// nothing there.  In a large one it is rounded, half a step of the type for each term of a sum, as a program would that
+// stores x a^T: the second plane's reads from the caches take 106 us instead of 89 in `outer` and 105 instead of 93 in `up`
+// (8192 rows, 4096 -> 16384, rank 64).
+// The values are laid out twice, in the order in which the lanes of `up` and of `outer` read them, padded to 16 rows.
+// Where there are not tiles enough for the compute units, workgroups share the summed dimension and leave parts of the sums,
+// in 32 bits: [splits][rows][padded].
 struct Hidden {
-    void *up;                   // [rows / 16][padded / EPL][16][EPL]
-    void *outer;                // 16 bits: [rows / 8][padded][8]; 32 bits: [rows][padded]
+    void *up;                   // [planes][rows / 16][padded / EPL][16][EPL]
+    void *outer;                // 16 bits: [planes][rows / 8][padded][8]; 32 bits: [rows][padded]
     float *parts;               // not null: what `down` leaves
-    u32 splits, padded;
+    u32 splits, padded, planes;
     bool folded;                // the parts are put together in `up` and `outer` before they are read
 };
 
@@ -171,6 +175,18 @@ DI u64 outer_place(u64 row, u32 j, u32 padded)
     return sizeof(T) == 4 ? row * padded + j : ((row >> 3) * padded + j) * 8 + (row & 7);
 }
 
+// elements of a plane
+DI u64 plane(u64 rows, u32 padded) { return (rows + 15) / 16 * 16 * padded; }
+
+// v as the sum of PLANES values of the type (where the first is an infinity the second adds nothing)
+template <class T>
+DI void in_planes(float v, T o[2])
+{
+    o[0] = (T)v;
+    const float left = v - (float)o[0];
+    o[1] = (T)(fabsf((float)o[0]) < INFINITY ? left : 0.f);
+}
+
 // four values of a row, from column `col` of the rank on
 template <class T>
 DI void store_hidden(const Hidden &h, const f32x4 &v, u64 row, u32 col, u32 split, u64 rows)
@@ -179,12 +195,22 @@ DI void store_hidden(const Hidden &h, const f32x4 &v, u64 row, u32 col, u32 spli
         *(f32x4 *)(h.parts + (split * rows + row) * h.padded + col) = v;
         return;
     }
-    typename Some<T, 4>::type o;
+    typename Some<T, 4>::type o[2];
 #pragma unroll
-    for (int e = 0; e < 4; e++) o[e] = (T)v[e];
-    *(typename Some<T, 4>::type *)((T *)h.up + up_place<T>(row, col, h.padded)) = o;
+    for (int e = 0; e < 4; e++) {
+        T both[2];
+        in_planes<T>(v[e], both);
+        o[0][e] = both[0];
+        o[1][e] = both[1];
+    }
 #pragma unroll
-    for (int e = 0; e < 4; e++) ((T *)h.outer)[outer_place<T>(row, col + e, h.padded)] = o[e];
+    for (int k = 0; k < Mma<T>::PLANES; k++) {
+        if (k && h.planes == 1) break;
+        const u64 from = k * plane(rows, h.padded);
+        *(typename Some<T, 4>::type *)((T *)h.up + from + up_place<T>(row, col, h.padded)) = o[k];
+#pragma unroll
+        for (int e = 0; e < 4; e++) ((T *)h.outer)[from + outer_place<T>(row, col + e, h.padded)] = o[k][e];
+    }
 }
 
 struct DownParams {
@@ -461,7 +487,7 @@ template <class T, int MR, int JS, int WR>
 __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
 {
     typedef typename Mma<T>::Frag Frag;
-    const int EPL = Mma<T>::EPL, STEP = Mma<T>::STEP, QN = EPL / 4, SLAB = SLAB_BYTES / sizeof(T), CPR = JS * STEP / EPL;
+    const int EPL = Mma<T>::EPL, STEP = Mma<T>::STEP, PLANES = Mma<T>::PLANES, QN = EPL / 4, SLAB = SLAB_BYTES / sizeof(T), CPR = JS * STEP / EPL;
     const int PANELS = 4 / WR, FILL = SLAB * CPR / (64 * WR);       // chunks of a panel that a lane fetches
     __shared__ Frag panel[WR == 4 ? 2 : 1][PANELS][SLAB * CPR];
     Tile t;
@@ -470,30 +496,26 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
     const u32 lane = lane_id(), m = lane & 15, group = lane >> 4, wave = wave_of_group();
     const u32 first = WR == 4 ? wave * MR * 16 : 0, rows = t.rows > first ? t.rows - first : 0, mine = WR == 4 ? 0 : wave;
     u32 col = (block % p.panels * p.trips * PANELS + mine) * SLAB;
-    if (t.adapter < 0) {
-        if (p.base == p.out) return;
-        T *const out = (T *)p.out + (u64)(t.row + first) * p.ldo;
-        const T *const base = p.base ? (const T *)p.base + (u64)(t.row + first) * p.ldb : nullptr;
-        for (u32 trip = 0; trip < p.trips; trip++, col += PANELS * SLAB)
-            for (u32 r = 0; r < min(rows, (u32)MR * 16); r++)
-                for (u32 c = col + lane; c < min(col + SLAB, p.cols); c += 64)
-                    out[r * p.ldo + c] = base ? base[r * p.ldb + c] : (T)0.f;
-        return;
-    }
+    const bool none = t.adapter < 0;
+    if (none && p.base == p.out) return;
     const u32 last = rows ? rows - 1 : 0;
     const u64 row0 = t.row + (rows ? first : 0);    // rows beyond the tile are its last one again, and not stored
-    Frag h[MR][JS];
+    Frag h[PLANES][MR][JS];
+    const bool two = PLANES == 2 && p.h.planes == 2;
 #pragma unroll
     for (int i = 0; i < MR; i++) {
         const u64 row = row0 + min(i * 16 + m, last);
+        if (none) break;
 #pragma unroll
         for (int s = 0; s < JS; s++) {
             const u32 j = s * STEP + group * EPL;
             if (j >= p.h.padded) {
 #pragma unroll
-                for (int e = 0; e < EPL; e++) h[i][s][e] = (T)0.f;
+                for (int k = 0; k < PLANES; k++) h[k][i][s] = Frag{};
             } else if (!p.h.parts) {
-                h[i][s] = *(const Frag *)((const T *)p.h.up + up_place<T>(row, j, p.h.padded));
+#pragma unroll
+                for (int k = 0; k < PLANES; k++)
+                    if (k == 0 || two) h[k][i][s] = *(const Frag *)((const T *)p.h.up + k * plane(p.q.rows, p.h.padded) + up_place<T>(row, j, p.h.padded));
             } else {
                 float v[EPL] = {};
                 const float *from = p.h.parts + row * p.h.padded + j;
@@ -505,11 +527,16 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
                         for (int k = 0; k < 4; k++) v[e + k] += f[k];
                     }
 #pragma unroll
-                for (int e = 0; e < EPL; e++) h[i][s][e] = (T)v[e];
+                for (int e = 0; e < EPL; e++) {
+                    T both[2];
+                    in_planes<T>(v[e], both);
+#pragma unroll
+                    for (int k = 0; k < PLANES; k++) h[k][i][s][e] = both[k];
+                }
             }
         }
     }
-    const T *const w = (const T *)p.w + (u64)t.adapter * p.cols * p.rank;
+    const T *const w = (const T *)p.w + (u64)(none ? 0 : t.adapter) * p.cols * p.rank;
     const char *const base = p.base ? (const char *)((const T *)p.base + row0 * p.ldb) : nullptr;
     char *const out = (char *)((T *)p.out + row0 * p.ldo);
     u32 yat[MR][4];
@@ -560,7 +587,7 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
         else
             wave_sync();
         if (!rows || col >= p.cols) continue;
-        if (base) {
+        if (base && !none) {
 #pragma unroll
             for (int i = 0; i < MR; i++) quad_swap(y[i]);
         }
@@ -568,6 +595,7 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
         // with EPL consecutive columns of one row in its register u, as it has them of y.
 #pragma unroll
         for (int u = 0; u < 4; u++) {
+            if (none) break;
             f32x4 acc[MR][QN];
 #pragma unroll
             for (int q = 0; q < QN; q++) {
@@ -578,7 +606,12 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
                 for (int s = 0; s < JS; s++) {
                     const Frag b = to[panel_place<CPR, SLAB / 4>(n, s * (STEP / EPL) + group)];
 #pragma unroll
-                    for (int i = 0; i < MR; i++) acc[i][q] = mma(b, h[i][s], acc[i][q]);
+                    for (int i = 0; i < MR; i++)
+acc[i][q] = mma(b, h[0][i][s], acc[i][q]);
+                    if (two) {
+#pragma unroll
+                        for (int i = 0; i < MR; i++) acc[i][q] = mma(b, h[PLANES - 1][i][s], acc[i][q]);
+                    }
                 }
             }
 #pragma unroll
@@ -589,9 +622,10 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
         const int n = (int)p.cols - (int)c;
 #pragma unroll
         for (int i = 0; i < MR; i++) {
-            quad_swap(y[i]);
+            if (!none) quad_swap(y[i]);
 #pragma unroll
             for (int u = 0; u < 4; u++) {
+                if (none && !base) y[i][u] = Frag{};
                 const u32 row = i * 16 + slab_row(lane, u);
                 if (row >= rows) continue;
                 T *const dst = (T *)(out + row * (u32)p.ldo * (u32)sizeof(T)) + c;
@@ -603,6 +637,78 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
                         if (e < n) dst[e] = y[i][u][e];
                 }
             }
+        }
+    }
+}
+
+// The same for requests of one token or two, where all there is to read is w: a lane has 16 bytes of it, the CPR lanes of a
+// column put their sums together, and a wavefront makes 64 columns at a time.  A chunk of the rank belongs to the same lane
+// in all of them, so its part of the (up to ROWS) rows' hidden values stays in registers, in 32 bits.
+const int FEW_ROWS = 4;
+
+template <class T, int CPR>
+__global__ __launch_bounds__(256) void lowrank_up_few_kernel(const UpParams p)
+{
+    typedef typename Mma<T>::Frag Frag;
+    const int EPL = Mma<T>::EPL;
+    Tile t;
+    const u32 block = die_order(blockIdx.x, gridDim.x);
+    if (!find_tile<FEW_ROWS>(p.q, block / p.panels, &t)) return;
+    const bool none = t.adapter < 0;
+    if (none && p.base == p.out) return;
+    const u32 lane = lane_id(), chunk = lane % CPR;
+    float h[FEW_ROWS][EPL];
+#pragma unroll
+    for (int r = 0; r < FEW_ROWS; r++) {
+        const u64 row = t.row + min((u32)r, t.rows - 1);
+#pragma unroll
+        for (int e = 0; e < EPL; e++) h[r][e] = 0.f;
+        if (none) continue;
+        if (p.h.parts) {
+            for (u32 u = 0; u < p.h.splits; u++) {
+                const float *from = p.h.parts + (u * (u64)p.q.rows + row) * p.h.padded + chunk * EPL;
+#pragma unroll
+                for (int e = 0; e < EPL; e++) h[r][e] += from[e];
+            }
+        } else {
+            for (u32 k = 0; k < p.h.planes; k++) {
+                const Frag f = *(const Frag *)((const T *)p.h.up + k * plane(p.q.rows, p.h.padded) + up_place<T>(row, chunk * EPL, p.h.padded));
+#pragma unroll
+                for (int e = 0; e < EPL; e++) h[r][e] += (float)f[e];
+            }
+        }
+    }
+    const T *const w = (const T *)p.w + (u64)(none ? 0 : t.adapter) * p.cols * p.rank;
+    u32 c0 = (block % p.panels * p.trips * 4 + wave_of_group()) * 64;
+    for (u32 trip = 0; trip < p.trips && c0 < p.cols; trip++, c0 += 256) {
+        Frag b[CPR];
+#pragma unroll
+        for (int i = 0; i < CPR; i++) {
+            const u32 col = c0 + (i * 64 + lane) / CPR;
+            b[i] = load_some<EPL>(w + (u64)min(col, p.cols - 1) * p.rank + chunk * EPL);
+        }
+        const u32 col = c0 + chunk * (64 / CPR) + lane / CPR;        // the one that this lane keeps
+        float y[FEW_ROWS], sum[FEW_ROWS];
+#pragma unroll
+        for (int r = 0; r < FEW_ROWS; r++) {
+            y[r] = sum[r] = 0.f;
+            if (p.base && (u32)r < t.rows && col < p.cols) y[r] = (float)((const T *)p.base)[(t.row + r) * p.ldb + col];
+        }
+#pragma unroll
+        for (int r = 0; r < FEW_ROWS; r++) {
+            if ((u32)r >= t.rows) break;
+#pragma unroll
+            for (int i = 0; i < CPR; i++) {
+                float v = 0.f;
+#pragma unroll
+                for (int e = 0; e < EPL; e++) v += h[r][e] * (float)b[i][e];
+                if (CPR > 1) v = dpp_add<DPP_QUAD_XOR1, 0xF>(v);
+                if (CPR > 2) v = dpp_add<DPP_QUAD_XOR2, 0xF>(v);
+                if (CPR > 4) v = dpp_add<DPP_ROW_HALF_MIRROR, 0xF>(v);
+                if (CPR > 8) v = dpp_add<DPP_ROW_MIRROR, 0xF>(v);
+                sum[r] = chunk == i ? v : sum[r];
+            }
+            if (col < p.cols) ((T *)p.out)[(t.row + r) * p.ldo + col] = (T)(none ? y[r] : y[r] + sum[r]);
         }
     }
 }
@@ -638,14 +744,24 @@ __global__ __launch_bounds__(256) void lowrank_fold_kernel(const FoldParams p)
     typedef typename Some<T, 4>::type Four;
 #pragma unroll
     for (int r = 0; r < 4; r++) {
-        Four o, c;
+        Four o[2], c[2];            // row + r, and in 16 bits the four rows of column col + r
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            o[e] = (T)v[r][e];
-            c[e] = sizeof(T) == 4 ? (T)v[r][e] : (T)v[e][r];        // 16 bits: four rows of column col + r
+            T both[2];
+            in_planes<T>(v[r][e], both);
+            o[0][e] = both[0];
+            o[1][e] = both[1];
+            in_planes<T>(sizeof(T) == 4 ? v[r][e] : v[e][r], both);
+            c[0][e] = both[0];
+            c[1][e] = both[1];
         }
-        if (up) *(Four *)((T *)h.up + up_place<T>(row + r, col, h.padded)) = o;
-        if (outer) *(Four *)((T *)h.outer + (sizeof(T) == 4 ? outer_place<T>(row + r, col, h.padded) : outer_place<T>(row, col + r, h.padded))) = c;
+#pragma unroll
+        for (int k = 0; k < Mma<T>::PLANES; k++) {
+            if (k && h.planes == 1) break;
+            const u64 from = k * plane(p.rows, h.padded);
+            if (up) *(Four *)((T *)h.up + from + up_place<T>(row + r, col, h.padded)) = o[k];
+            if (outer) *(Four *)((T *)h.outer + from + (sizeof(T) == 4 ? outer_place<T>(row + r, col, h.padded) : outer_place<T>(row, col + r, h.padded))) = c[k];
+        }
     }
 }
 
@@ -658,6 +774,7 @@ struct OuterJob {
 struct OuterParams {
     OuterJob job[2];
     Requests q;
+    u32 planes;
 };
 
 // two 16-bit elements of each of two registers, swapped: (a0 b0) and (a1 b1) of (a0 a1), (b0 b1)
@@ -667,7 +784,7 @@ DI u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302
 // Rows t to t + 31 of CQ columns a lane, and what belongs to them of hidden; 0 in the place of rows that are not from lo to
 // hi - 1, whatever lies there.  t is a multiple of 8.  WHOLE: all of these rows, and whole panels.
 template <class T, int CQ, int NR, bool WHOLE>
-DI void outer_load(const OuterJob &o, u32 t, u32 lo, u32 hi, u32 col, int cols, u32 (&v)[8][CQ / 2], typename Mma<T>::Frag (&h)[NR])
+DI void outer_load(const OuterJob &o, u32 t, u32 lo, u32 hi, u32 rows, u32 col, int cols, u32 (&v)[8][CQ / 2], typename Mma<T>::Frag (&h)[2][NR], bool two)
 {
     typedef typename Mma<T>::Frag Frag;
     const u32 lane = lane_id(), m = lane & 15, r0 = t + (lane >> 4) * 8;
@@ -682,20 +799,25 @@ DI void outer_load(const OuterJob &o, u32 t, u32 lo, u32 hi, u32 col, int cols, 
         __builtin_memcpy(v[e], &x, sizeof x);
     }
 #pragma unroll
-    for (int j = 0; j < NR; j++) {
-        h[j] = Frag{};
-        if (WHOLE || (r0 + 8 > lo && r0 < hi)) h[j] = *(const Frag *)((const T *)o.hidden + outer_place<T>(r0, j * 16 + m, NR * 16));
-        if (!WHOLE) {
+    for (int k = 0; k < 2; k++) {
+        if (k && !two) break;
 #pragma unroll
-            for (int e = 0; e < 8; e++)
-                if (r0 + e < lo || r0 + e >= hi) h[j][e] = (T)0.f;
+        for (int j = 0; j < NR; j++) {
+            h[k][j] = Frag{};
+            if (WHOLE || (r0 + 8 > lo && r0 < hi))
+                h[k][j] = *(const Frag *)((const T *)o.hidden + k * plane(rows, NR * 16) + outer_place<T>(r0, j * 16 + m, NR * 16));
+            if (!WHOLE) {
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if (r0 + e < lo || r0 + e >= hi) h[k][j][e] = (T)0.f;
+            }
         }
     }
 }
 
 // acc[q][j] += v^T hidden for column q of a lane and the j-th 16 of the rank
 template <class T, int CQ, int NR>
-DI void outer_add(const u32 (&v)[8][CQ / 2], const typename Mma<T>::Frag (&h)[NR], f32x4 (&acc)[CQ][NR])
+DI void outer_add(const u32 (&v)[8][CQ / 2], const typename Mma<T>::Frag (&h)[2][NR], bool two, f32x4 (&acc)[CQ][NR])
 {
     typedef typename Mma<T>::Frag Frag;
 #pragma unroll
@@ -711,8 +833,15 @@ DI void outer_add(const u32 (&v)[8][CQ / 2], const typename Mma<T>::Frag (&h)[NR
         __builtin_memcpy(&b, high, sizeof b);
 #pragma unroll
         for (int j = 0; j < NR; j++) {
-            acc[q][j] = mma(a, h[j], acc[q][j]);
-            acc[q + 1][j] = mma(b, h[j], acc[q + 1][j]);
+            acc[q][j] = mma(a, h[0][j], acc[q][j]);
+            acc[q + 1][j] = mma(b, h[0][j], acc[q + 1][j]);
+        }
+        if (two) {
+#pragma unroll
+            for (int j = 0; j < NR; j++) {
+                acc[q][j] = mma(a, h[1][j], acc[q][j]);
+                acc[q + 1][j] = mma(b, h[1][j], acc[q + 1][j]);
+            }
         }
     }
 }
@@ -796,12 +925,12 @@ __global__ __launch_bounds__(256) void lowrank_outer_kernel(const OuterParams p)
                     outer_add32<CQ, NR>(v, h, acc);
                 } else {
                     u32 v[8][CQ / 2];
-                    typename Mma<T>::Frag h[NR];
+                    typename Mma<T>::Frag h[2][NR];
                     if (LIKELY(whole))
-                        outer_load<T, CQ, NR, true>(o, t, begin, end, col, cols, v, h);
+                        outer_load<T, CQ, NR, true>(o, t, begin, end, p.q.rows, col, cols, v, h, p.planes == 2);
                     else
-                        outer_load<T, CQ, NR, false>(o, t, begin, end, col, cols, v, h);
-                    outer_add<T, CQ, NR>(v, h, acc);
+                        outer_load<T, CQ, NR, false>(o, t, begin, end, p.q.rows, col, cols, v, h, p.planes == 2);
+                    outer_add<T, CQ, NR>(v, h, p.planes == 2, acc);
                 }
             }
         }
@@ -848,7 +977,17 @@ __global__ __launch_bounds__(256) void lowrank_join_kernel(const JoinParams p)
     for (int e = 0; e < 8; e++) v[e] = 0.f;
     const u64 apart = (u64)gridDim.z * p.padded * o.cols;
     const float *from = o.sums + ((u64)adapter * p.padded + j) * o.cols + c;
-    for (u32 u = 0; u < o.chunks; u++, from += apart)
+    u32 u = 0;
+    for (; u + 4 <= o.chunks; u += 4, from += 4 * apart) {      // four chunks' loads under way at a time
+        float f[4][8];
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) f[k][e] = from[k * apart + (u64)e * o.cols];
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] += (f[0][e] + f[1][e]) + (f[2][e] + f[3][e]);
+    }
+    for (; u < o.chunks; u++, from += apart)
 #pragma unroll
         for (int e = 0; e < 8; e++) v[e] += from[(u64)e * o.cols];
     if (o.transposed) {
@@ -940,7 +1079,10 @@ Cut cut_of(const vms_lowrank_args *a, u64 in)
     return c;
 }
 
-size_t laid_out(const vms_lowrank_args *a) { return (a->rows + 15) / 16 * 16 * padded_rank(a->rank) * type_bytes(a->dtype); }
+u32 planes_of(const vms_lowrank_args *a) { return a->dtype != VMS_F32 && a->rows * a->rank <= 1 << 16 ? 2 : 1; }
+
+// bytes of one layout with its planes
+size_t laid_out(const vms_lowrank_args *a) { return (a->rows + 15) / 16 * 16 * padded_rank(a->rank) * type_bytes(a->dtype) * planes_of(a); }
 
 size_t parts_bytes(const vms_lowrank_args *a, const Cut &c) { return c.splits > 1 ? (size_t)c.splits * a->rows * padded_rank(a->rank) * 4 : 0; }
 bool folded(const Cut &c) { return c.splits > 1 && c.tile16 == 8; }
@@ -949,11 +1091,11 @@ size_t hidden_bytes(const vms_lowrank_args *a, const Cut &c) { return (c.splits 
 
 Hidden hidden_at(const vms_lowrank_args *a, const Cut &c, void *at)
 {
-    const u32 padded = padded_rank(a->rank);
+    const u32 padded = padded_rank(a->rank), planes = planes_of(a);
     char *const p = (char *)at;
-    if (c.splits == 1) return Hidden{ p, p + laid_out(a), nullptr, 1, padded, false };
-    if (folded(c)) return Hidden{ p, p + laid_out(a), (float *)(p + 2 * laid_out(a)), c.splits, padded, true };
-    return Hidden{ nullptr, nullptr, (float *)p, c.splits, padded, false };
+    if (c.splits == 1) return Hidden{ p, p + laid_out(a), nullptr, 1, padded, planes, false };
+    if (folded(c)) return Hidden{ p, p + laid_out(a), (float *)(p + 2 * laid_out(a)), c.splits, padded, planes, true };
+    return Hidden{ nullptr, nullptr, (float *)p, c.splits, padded, planes, false };
 }
 
 int check(const vms_lowrank_args *a)
@@ -1036,17 +1178,40 @@ int launch_up(const UpParams &p, u32 grid, void *stream)
     case 32: return ops_launch(lowrank_up_kernel<T, MR, 32 / per, WR>, dim3(grid), block, 0, p, stream);
     case 64: return ops_launch(lowrank_up_kernel<T, MR, 64 / per, WR>, dim3(grid), block, 0, p, stream);
     }
-    return ops_launch(lowrank_up_kernel<T, MR, 128 / per, WR>, dim3(grid), block, 0, p, stream);
+    return ops_launch(lowrank_up_kernel<T, 1, 128 / per, WR>, dim3(grid), block, 0, p, stream);
+}
+
+template <class T>
+int up_few(const vms_lowrank_args *a, const Hidden &h, const void *w, const void *base, u64 ldb, void *out, u64 ldo, u64 cols, u32 tiles, void *stream)
+{
+    const u64 all = (cols + 255) / 256;
+    u64 trips = (all * tiles + OPS_CUS * 4 - 1) / (OPS_CUS * 4);
+    trips = trips > 8 ? 8 : trips;
+    const UpParams p = { h, w, base, out, requests_of(a), ldb, ldo, (u32)cols, a->rank, (u32)trips, (u32)((all + trips - 1) / trips) };
+    const dim3 grid(tiles * p.panels), block(256);
+    switch (a->rank / Mma<T>::EPL) {
+    case 1: return ops_launch(lowrank_up_few_kernel<T, 1>, grid, block, 0, p, stream);
+    case 2: return ops_launch(lowrank_up_few_kernel<T, 2>, grid, block, 0, p, stream);
+    case 4: return ops_launch(lowrank_up_few_kernel<T, 4>, grid, block, 0, p, stream);
+    case 8: return ops_launch(lowrank_up_few_kernel<T, 8>, grid, block, 0, p, stream);
+    }
+    return ops_launch(lowrank_up_few_kernel<T, 16>, grid, block, 0, p, stream);
 }
 
 template <class T>
 int up(const vms_lowrank_args *a, const Hidden &h, const void *w, const void *base, u64 ldb, void *out, u64 ldo, u64 cols, void *stream)
 {
     const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
-    const u32 tile16 = each >= 512 ? 8 : each >= 48 ? 4 : 1, tiles = (u32)tiles_of(a, tile16);
+    const u32 chunks = a->rank / Mma<T>::EPL;
+    if (each <= 2 && a->rank % Mma<T>::EPL == 0 && chunks <= 16 && (chunks & (chunks - 1)) == 0) {
+        const u64 tiles = a->d_starts ? a->rows / FEW_ROWS + requests + 2 : (a->rows + FEW_ROWS - 1) / FEW_ROWS;
+        return up_few<T>(a, h, w, base, ldb, out, ldo, cols, (u32)(tiles < a->rows ? tiles : a->rows), stream);
+    }
+    const u32 tile16 = each >= 512 && a->rank <= 64 ? 8 : each >= 48 ? 4 : 1, tiles = (u32)tiles_of(a, tile16);
     const u64 trip = (tile16 == 1 ? 4 : 1) * SLAB_BYTES / sizeof(T), all = (cols + trip - 1) / trip;
-    // workgroups enough for four on every compute unit before one takes a second trip
-    u64 trips = all * tiles / (OPS_CUS * 4);
+    // Workgroups enough for four on every compute unit before one takes a second trip; no more than that where each has to
+    // find its request first (24 requests, 6007 rows, 4096 -> 4096, rank 32: 22 us, 25 with as many again).
+    u64 trips = (all * tiles + (a->d_starts ? OPS_CUS * 4 - 1 : 0)) / (OPS_CUS * 4);
     trips = trips < 1 ? 1 : trips > 8 ? 8 : trips;
     const UpParams p = { h, w, base, out, requests_of(a), ldb, ldo, (u32)cols, a->rank, (u32)trips, (u32)((all + trips - 1) / trips) };
     const u32 grid = tiles * p.panels;
@@ -1146,7 +1311,7 @@ int backward(const vms_lowrank_backward_args *a, void *stream)
         rc = fold<T>(some, stream);
         if (rc) return rc;
     }
-    OuterParams o = { { l.da, l.db }, requests_of(&f) };
+    OuterParams o = { { l.da, l.db }, requests_of(&f), h.planes };
     o.job[0].v = f.d_x;
     o.job[0].ldv = f.ldx;
     o.job[0].hidden = dh.outer;

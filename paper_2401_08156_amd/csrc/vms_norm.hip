@@ -35,38 +35,33 @@ struct NormJoinParams {
     u32 parts, cols;
 };
 
-// The sums over the lanes that share a row: of a wavefront, or of the workgroup through `part`, which two
-// uses in a row must not share (the barrier between them lies in front of the second's reads).
-template <int LANES>
-DI float row_sum(float v, float *part)
+// The sum over a workgroup's lanes, through `part`, which two uses in a row must not share (the barrier between them lies in
+// front of the second's reads).
+DI float group_sum(float v, float *part)
 {
     v = wave_sum(v);
-    if (LANES == 64) return v;
-    const u32 wave = wave_of_group();
-    if (lane_id() == 0) part[wave] = v;
+    if (lane_id() == 0) part[wave_of_group()] = v;
     __syncthreads();
-    v = 0.f;
-#pragma unroll
-    for (int w = 0; w < LANES / 64; w++) v += part[w];
-    return v;
+    const u32 k = threadIdx.x & 15;
+    return row16_sum(k < blockDim.x / 64 ? part[k] : 0.f);
 }
 
 // s of eight columns: x, or residual + dropout(x)
-template <class T>
+template <class T, bool ONCE>
 DI void norm_input(const NormParams &p, u64 seed, u32 row, u32 group, float v[8])
 {
     const u32 col = group * 8, n = p.cols - col;
-    load8((const T *)p.x + row * p.ldx + col, n, v);
+    load8<ONCE>((const T *)p.x + row * p.ldx + col, n, v);
     if (p.residual) {
         float r[8];
-        load8((const T *)p.residual + row * p.ldr + col, n, r);
+        load8<ONCE>((const T *)p.residual + row * p.ldr + col, n, r);
         if (p.mask.limit) drop8(p.mask, seed, row, group, v);
 #pragma unroll
         for (int i = 0; i < 8; i++) v[i] += r[i];
     }
 }
 
-template <class T>
+template <class T, bool ONCE>
 DI void norm_output(const NormParams &p, u32 row, u32 group, const float v[8], float mean, float rstd)
 {
     const u32 col = group * 8, n = p.cols - col;
@@ -79,13 +74,13 @@ DI void norm_output(const NormParams &p, u32 row, u32 group, const float v[8], f
         if (p.weight) o[i] *= w[i];
         if (p.bias) o[i] += b[i];
     }
-    store8((T *)p.y + row * p.ldy + col, n, o);
-    if (p.s) store8((T *)p.s + row * p.lds + col, n, v);
+    store8<ONCE>((T *)p.y + row * p.ldy + col, n, o);
+    if (p.s) store8<ONCE>((T *)p.s + row * p.lds + col, n, v);
 }
 
 // Sum and squares around the mean of a row's part in a wavefront; `mine` columns, the other places hold 0.
-template <int LANES, int NG>
-DI void part_stats(const float v[NG][8], u32 lane, u32 cols, u32 mine, float *sum, float *m2)
+template <int NG>
+DI void part_stats(const float v[NG][8], const u32 n[NG], u32 mine, float *sum, float *m2)
 {
     float a = 0.f, b = 0.f;
 #pragma unroll
@@ -96,111 +91,110 @@ DI void part_stats(const float v[NG][8], u32 lane, u32 cols, u32 mine, float *su
     const float mean = mine ? a / (float)mine : 0.f;
 #pragma unroll
     for (int g = 0; g < NG; g++) {
-        const u32 col = (g * LANES + lane) * 8;
+        if (LIKELY(n[g] >= 8)) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const float d = v[g][i] - mean;
-            if (col + i < cols) b += d * d;
+            for (int i = 0; i < 8; i++) {
+                const float d = v[g][i] - mean;
+                b += d * d;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float d = v[g][i] - mean;
+                if ((u32)i < n[g]) b += d * d;
+            }
         }
     }
     *sum = a;
     *m2 = wave_sum(b);
 }
 
-// mean and 1 / sqrt(variance + eps) of a row from its parts
-template <int PARTS>
-DI void join_stats(const float *sum, const float *m2, const float *n, u32 cols, float eps, float *mean, float *rstd)
+// mean and 1 / sqrt(variance + eps) of a row from its parts, one in each lane of 16
+DI void join_stats(float sum, float m2, float n, u32 cols, float eps, float *mean, float *rstd)
 {
-    float total = 0.f, squares = 0.f;
-#pragma unroll
-    for (int w = 0; w < PARTS; w++) total += sum[w];
-    *mean = total / (float)cols;
-#pragma unroll
-    for (int w = 0; w < PARTS; w++) {
-        const float d = n[w] > 0.f ? sum[w] / n[w] - *mean : 0.f;
-        squares += m2[w] + n[w] * d * d;
-    }
-    *rstd = 1.f / sqrtf(squares / (float)cols + eps);
+    *mean = row16_sum(sum) / (float)cols;
+    const float d = n > 0.f ? sum / n - *mean : 0.f;
+    *rstd = 1.f / sqrtf(row16_sum(m2 + n * d * d) / (float)cols + eps);
 }
 
-// A row in the registers of LANES lanes, NG groups each; 64: four rows a workgroup.
+// A row in the registers of a workgroup, NG groups a lane; SINGLE: of a wavefront, four rows a workgroup.
 //
 // y goes by the sum s as it is in 32 bits.  The statistics for the backward pass are those of s rounded to the type,
 // which is what that pass reads: with the others a row of small variance, whose rstd is large, would get a gradient of
 // rounding errors, (s rounded - mean) * rstd.
-template <class T, int LANES, int NG>
-__global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void norm_kernel(const NormParams p)
+template <class T, bool SINGLE, int NG, bool ONCE>
+__global__ __launch_bounds__(SINGLE ? 256 : 1024) void norm_kernel(const NormParams p)
 {
-    const int PARTS = LANES / 64;
-    __shared__ float parts[2][5][PARTS];
-    const u32 lane = LANES == 64 ? lane_id() : threadIdx.x, wave = wave_of_group();
-    const u32 step = LANES == 64 ? gridDim.x * 4 : gridDim.x;
+    __shared__ float parts[2][5][16];
+    const u32 lanes = SINGLE ? 64 : blockDim.x, lane = SINGLE ? lane_id() : threadIdx.x, wave = wave_of_group(), waves = lanes / 64;
+    const u32 step = SINGLE ? gridDim.x * 4 : gridDim.x;
     const bool rounded = sizeof(T) == 2 && p.s && p.stats;
     u32 odd = 0;
     const u64 seed = p.mask.limit ? mask_seed(p.mask) : 0;
-    // columns of this wavefront: those of the groups that its lanes have
-    const u32 first = LANES == 64 ? 0 : wave * 64;
-    u32 mine = 0;
+    u32 n[NG], mine = 0;            // columns of a lane's groups, and of all groups of this wavefront
 #pragma unroll
     for (int g = 0; g < NG; g++) {
-        const u32 at = (g * LANES + first) * 8;
+        const u32 col = (g * lanes + lane) * 8, at = (g * lanes + (SINGLE ? 0 : wave * 64)) * 8;
+        n[g] = p.cols > col ? p.cols - col : 0;
         mine += p.cols > at ? min(p.cols - at, 512u) : 0u;
     }
-    for (u32 row = LANES == 64 ? blockIdx.x * 4 + wave : blockIdx.x; row < p.rows; row += step) {
+    for (u32 row = SINGLE ? blockIdx.x * 4 + wave : blockIdx.x; row < p.rows; row += step) {
         float v[NG][8];
 #pragma unroll
         for (int g = 0; g < NG; g++) {
-            const u32 group = g * LANES + lane;
 #pragma unroll
             for (int i = 0; i < 8; i++) v[g][i] = 0.f;
-            if (group < p.groups) norm_input<T>(p, seed, row, group, v[g]);
+            if (n[g]) norm_input<T, ONCE>(p, seed, row, g * lanes + lane, v[g]);
         }
-        float(&part)[5][PARTS] = parts[odd];        // two places in turn: a wavefront may be one row ahead, not two
-        odd ^= 1;
-        float sum, m2, n = (float)mine;
-        part_stats<LANES, NG>(v, lane, p.cols, mine, &sum, &m2);
-        if (PARTS > 1 && lane_id() == 0) {
-            part[0][wave] = sum;
-            part[1][wave] = m2;
-            part[2][wave] = n;
-        }
-        float sum2 = 0.f, m22 = 0.f;
+        float sum, m2, sum2 = 0.f, m22 = 0.f;
+        part_stats<NG>(v, n, mine, &sum, &m2);
         if (rounded) {
             float r[NG][8];
 #pragma unroll
             for (int g = 0; g < NG; g++)
 #pragma unroll
                 for (int i = 0; i < 8; i++) r[g][i] = (float)(T)v[g][i];
-            part_stats<LANES, NG>(r, lane, p.cols, mine, &sum2, &m22);
-            if (PARTS > 1 && lane_id() == 0) {
+            part_stats<NG>(r, n, mine, &sum2, &m22);
+        }
+        float count = (float)mine;
+        if (SINGLE) {               // one part
+            const bool one = (lane & 15) == 0;
+            sum = one ? sum : 0.f;
+            m2 = one ? m2 : 0.f;
+            sum2 = one ? sum2 : 0.f;
+            m22 = one ? m22 : 0.f;
+            count = one ? count : 0.f;
+        } else {
+            float(&part)[5][16] = parts[odd];       // two places in turn: a wavefront may be one row ahead, not two
+            odd ^= 1;
+            if (lane_id() == 0) {
+                part[0][wave] = sum;
+                part[1][wave] = m2;
+                part[2][wave] = count;
                 part[3][wave] = sum2;
                 part[4][wave] = m22;
             }
-        }
-        float mean, rstd, mean2, rstd2;
-        if (PARTS > 1) {
             __syncthreads();
-            join_stats<PARTS>(part[0], part[1], part[2], p.cols, p.eps, &mean, &rstd);
-        } else {
-            join_stats<1>(&sum, &m2, &n, p.cols, p.eps, &mean, &rstd);
+            const u32 w = lane & 15;
+            sum = w < waves ? part[0][w] : 0.f;
+            m2 = w < waves ? part[1][w] : 0.f;
+            count = w < waves ? part[2][w] : 0.f;
+            sum2 = w < waves ? part[3][w] : 0.f;
+            m22 = w < waves ? part[4][w] : 0.f;
         }
-        if (p.stats && lane == 0) {
-            mean2 = mean;
-            rstd2 = rstd;
-            if (rounded) {
-                if (PARTS > 1)
-                    join_stats<PARTS>(part[3], part[4], part[2], p.cols, p.eps, &mean2, &rstd2);
-                else
-                    join_stats<1>(&sum2, &m22, &n, p.cols, p.eps, &mean2, &rstd2);
+        float mean, rstd;
+        join_stats(sum, m2, count, p.cols, p.eps, &mean, &rstd);
+        if (p.stats) {
+            float mean2 = mean, rstd2 = rstd;
+            if (rounded) join_stats(sum2, m22, count, p.cols, p.eps, &mean2, &rstd2);
+            if (lane == 0) {
+                p.stats[(u64)row * 2] = mean2;
+                p.stats[(u64)row * 2 + 1] = rstd2;
             }
-            p.stats[(u64)row * 2] = mean2;
-            p.stats[(u64)row * 2 + 1] = rstd2;
         }
 #pragma unroll
-        for (int g = 0; g < NG; g++) {
-            const u32 group = g * LANES + lane;
-            if (group < p.groups) norm_output<T>(p, row, group, v[g], mean, rstd);
-        }
+        for (int g = 0; g < NG; g++)
+            if (n[g]) norm_output<T, ONCE>(p, row, g * lanes + lane, v[g], mean, rstd);
     }
 }
 
@@ -217,7 +211,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p)
         for (int pass = 0; pass < 2; pass++) {
             float acc[2] = {};
             for (u32 group = threadIdx.x; group < p.groups; group += 1024) {
-                norm_input<T>(p, seed, row, group, v);
+                norm_input<T, false>(p, seed, row, group, v);
                 const u32 n = p.cols - group * 8;
                 float one[2] = {};              // sums of sums: the rounding errors of a long row stay small
 #pragma unroll
@@ -232,8 +226,8 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p)
                 acc[1] += one[1];
             }
             float *const to = pass ? m2 : mean;
-            to[0] = row_sum<1024>(acc[0], part[pass * 2]) / (float)p.cols;
-            to[1] = row_sum<1024>(acc[1], part[pass * 2 + 1]) / (float)p.cols;
+            to[0] = group_sum(acc[0], part[pass * 2]) / (float)p.cols;
+            to[1] = group_sum(acc[1], part[pass * 2 + 1]) / (float)p.cols;
         }
         const float rstd = 1.f / sqrtf(m2[0] + p.eps);
         if (p.stats && threadIdx.x == 0) {
@@ -241,8 +235,8 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p)
             p.stats[(u64)row * 2 + 1] = 1.f / sqrtf(m2[rounded] + p.eps);
         }
         for (u32 group = threadIdx.x; group < p.groups; group += 1024) {
-            norm_input<T>(p, seed, row, group, v);
-            norm_output<T>(p, row, group, v, mean[0], rstd);
+            norm_input<T, false>(p, seed, row, group, v);
+            norm_output<T, false>(p, row, group, v, mean[0], rstd);
         }
     }
 }
@@ -266,104 +260,125 @@ DI void back_weight(const NormBackParams &p, u32 group, float w[8])
     if (p.weight) load8((const T *)p.weight + group * 8, p.cols - group * 8, w);
 }
 
-template <class T>
+template <class T, bool ONCE>
 DI void back_output(const NormBackParams &p, u64 seed, u32 row, u32 group, const float dy[8], const float h[8], const float w[8],
-                    float rstd, float c1, float c2)
+                    const typename Eight<T>::type &ds, float rstd, float c1, float c2)
 {
     const u32 col = group * 8, n = p.cols - col;
     float o[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) o[i] = rstd * (dy[i] * w[i] - c1 - h[i] * c2);
     if (p.ds) {
-        float e[8];
-        load8((const T *)p.ds + row * p.ldds + col, n, e);
 #pragma unroll
-        for (int i = 0; i < 8; i++) o[i] += e[i];
+        for (int i = 0; i < 8; i++) o[i] += (float)ds[i];
     }
-    store8((T *)p.dres + row * p.lddres + col, n, o);
+    store8<ONCE>((T *)p.dres + row * p.lddres + col, n, o);
     if (p.dx) {
         if (p.mask.limit) drop8(p.mask, seed, row, group, o);
-        store8((T *)p.dx + row * p.lddx + col, n, o);
+        store8<ONCE>((T *)p.dx + row * p.lddx + col, n, o);
     }
 }
 
-// A workgroup takes every gridDim.x-th row (64 lanes: four rows at a time) and keeps the sums for the weights'
+// A workgroup takes every gridDim.x-th row (SINGLE: four rows at a time, a wavefront each) and keeps the sums for the weights'
 // gradients in registers until its last row.
-template <class T, int LANES, int NG, bool WEIGHTS>
-__global__ __launch_bounds__(LANES == 64 ? 256 : LANES) void norm_back_kernel(const NormBackParams p)
+template <class T, bool SINGLE, int NG, bool WEIGHTS, bool ONCE>
+__global__ __launch_bounds__(SINGLE ? 256 : 1024) void norm_back_kernel(const NormBackParams p)
 {
-    __shared__ float part[2][2][LANES / 64];
-    __shared__ float joined[LANES == 64 && WEIGHTS ? 4 * 64 * 8 : 1];
-    const u32 lane = LANES == 64 ? lane_id() : threadIdx.x;
-    const u32 first = LANES == 64 ? blockIdx.x * 4 + wave_of_group() : blockIdx.x;
-    const u32 step = LANES == 64 ? gridDim.x * 4 : gridDim.x;
+    __shared__ float part[2][2][16];
+    __shared__ float joined[SINGLE && WEIGHTS ? 4 * 64 * 8 : 1];
+    const u32 lanes = SINGLE ? 64 : blockDim.x, lane = SINGLE ? lane_id() : threadIdx.x, waves = lanes / 64;
+    const u32 first = SINGLE ? blockIdx.x * 4 + wave_of_group() : blockIdx.x;
+    const u32 step = SINGLE ? gridDim.x * 4 : gridDim.x;
     const u64 seed = p.mask.limit ? mask_seed(p.mask) : 0;
     float w[NG][8], dw[WEIGHTS ? NG : 1][8], db[WEIGHTS ? NG : 1][8];
 #pragma unroll
     for (int g = 0; g < NG; g++) {
-        const u32 group = g * LANES + lane;
+        const u32 group = g * lanes + lane;
         if (group < p.groups) back_weight<T>(p, group, w[g]);
 #pragma unroll
         for (int i = 0; i < 8; i++)
             if (WEIGHTS) dw[g][i] = db[g][i] = 0.f;
     }
+    // With one group a lane, what a row's gradient is made of is read while the row before it is worked on (131 us for 16384 x
+    // 4096 in 16 bits with residual and dropout, 141 without); the registers do not hold two rows of two.
+    const bool AHEAD = NG == 1;
+    typedef typename Eight<T>::type Raw;
+    Raw dy2 = {}, s2 = {}, ds2 = {};
+    const auto fetch = [&](u32 row) {
+        const u32 col = lane * 8, n = p.cols - col;
+        if (lane >= p.groups) return;
+        dy2 = load8_raw<ONCE>((const T *)p.dy + row * p.lddy + col, n);
+        s2 = load8_raw<ONCE>((const T *)p.s + row * p.lds + col, n);
+        if (p.ds) ds2 = load8_raw<ONCE>((const T *)p.ds + row * p.ldds + col, n);
+    };
+    if (AHEAD && first < p.rows) fetch(first);
     u32 odd = 0;
     for (u32 row = first; row < p.rows; row += step) {
         const float mean = p.stats[(u64)row * 2], rstd = p.stats[(u64)row * 2 + 1];
         float dy[NG][8], h[NG][8];
+        Raw ds = ds2;
         float c1 = 0.f, c2 = 0.f;
 #pragma unroll
         for (int g = 0; g < NG; g++) {
-            const u32 group = g * LANES + lane;
+            const u32 group = g * lanes + lane, col = group * 8, n = p.cols - col;
 #pragma unroll
             for (int i = 0; i < 8; i++) dy[g][i] = h[g][i] = 0.f;
-            if (group < p.groups) {
-                back_input<T>(p, row, group, mean, rstd, dy[g], h[g]);
+            if (group >= p.groups) continue;
+            if (AHEAD) {
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    const float e = dy[g][i] * w[g][i];
-                    c1 += e;
-                    c2 += e * h[g][i];
-                    if (WEIGHTS) {
-                        dw[g][i] += dy[g][i] * h[g][i];
-                        db[g][i] += dy[g][i];
-                    }
+                    dy[g][i] = (float)dy2[i];
+                    h[g][i] = (float)s2[i];
+                }
+            } else {
+                load8<ONCE>((const T *)p.dy + row * p.lddy + col, n, dy[g]);
+                load8<ONCE>((const T *)p.s + row * p.lds + col, n, h[g]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                h[g][i] = (u32)i < n ? (h[g][i] - mean) * rstd : 0.f;
+                const float e = dy[g][i] * w[g][i];
+                c1 += e;
+                c2 += e * h[g][i];
+                if (WEIGHTS) {
+                    dw[g][i] += dy[g][i] * h[g][i];
+                    db[g][i] += dy[g][i];
                 }
             }
         }
+        if (AHEAD && row + step < p.rows) fetch(row + step);
         c1 = wave_sum(c1);
         c2 = wave_sum(c2);
-        if (LANES > 64) {           // two places in turn: a wavefront may be one row ahead, not two
+        if (!SINGLE) {              // two places in turn: a wavefront may be one row ahead, not two
             if (lane_id() == 0) {
                 part[odd][0][wave_of_group()] = c1;
                 part[odd][1][wave_of_group()] = c2;
             }
             __syncthreads();
-            c1 = c2 = 0.f;
-#pragma unroll
-            for (int i = 0; i < LANES / 64; i++) {
-                c1 += part[odd][0][i];
-                c2 += part[odd][1][i];
-            }
+            const u32 k = lane & 15;
+            c1 = row16_sum(k < waves ? part[odd][0][k] : 0.f);
+            c2 = row16_sum(k < waves ? part[odd][1][k] : 0.f);
             odd ^= 1;
         }
         c1 /= (float)p.cols;
         c2 /= (float)p.cols;
 #pragma unroll
         for (int g = 0; g < NG; g++) {
-            const u32 group = g * LANES + lane;
-            if (group < p.groups) back_output<T>(p, seed, row, group, dy[g], h[g], w[g], rstd, c1, c2);
+            const u32 group = g * lanes + lane;
+            if (group >= p.groups) continue;
+            if (!AHEAD && p.ds) ds = load8_raw<ONCE>((const T *)p.ds + row * p.ldds + group * 8, p.cols - group * 8);
+            back_output<T, ONCE>(p, seed, row, group, dy[g], h[g], w[g], ds, rstd, c1, c2);
         }
     }
     if (WEIGHTS) {
         float *out = p.partial + (u64)blockIdx.x * 2 * p.cols;
 #pragma unroll
         for (int g = 0; g < NG; g++) {
-            const u32 group = g * LANES + lane;
+            const u32 group = g * lanes + lane;
 #pragma unroll
             for (int k = 0; k < 2; k++) {
                 float(&v)[8] = k ? db[g] : dw[g];
-                if (LANES == 64) {      // the four wavefronts' sums
+                if (SINGLE) {      // the four wavefronts' sums
                     __syncthreads();
 #pragma unroll
                     for (int i = 0; i < 8; i++) joined[(wave_of_group() * 8 + i) * 64 + lane] = v[i];
@@ -424,13 +439,15 @@ __global__ __launch_bounds__(1024) void norm_back_long_kernel(const NormBackPara
             }
         }
         begun = true;
-        c1 = row_sum<1024>(c1, part[odd]) / (float)p.cols;
-        c2 = row_sum<1024>(c2, part[odd + 1]) / (float)p.cols;
+        c1 = group_sum(c1, part[odd]) / (float)p.cols;
+        c2 = group_sum(c2, part[odd + 1]) / (float)p.cols;
         odd ^= 2;
         for (u32 group = threadIdx.x; group < p.groups; group += 1024) {
             back_input<T>(p, row, group, mean, rstd, dy, h);
             back_weight<T>(p, group, w);
-            back_output<T>(p, seed, row, group, dy, h, w, rstd, c1, c2);
+            typename Eight<T>::type ds = {};
+            if (p.ds) ds = load8_raw((const T *)p.ds + row * p.ldds + group * 8, p.cols - group * 8);
+            back_output<T, false>(p, seed, row, group, dy, h, w, ds, rstd, c1, c2);
         }
     }
 }
@@ -466,43 +483,40 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const NormJoinParams p)
     }
 }
 
-template <class T>
+// Which registers hold a row: those of a wavefront up to 1024 columns, those of a workgroup of as many wavefronts as it needs
+// up to 16384 (two groups a lane; to 32768 with four), none beyond.  A workgroup for each row: many of them at different stages
+// keep the memory busier than ones that stay and read a row ahead, of which fewer fit (122 and 131 us for 16384 x 4096 in 16 bits).
+template <class T, bool ONCE>
 int launch_norm(const NormParams &p, void *stream)
 {
     const u32 g = p.groups, most = 1u << 18;      // workgroups; they go on to further rows
     const dim3 quarter(p.rows / 4 < most ? (p.rows + 3) / 4 : most), each(p.rows < most ? p.rows : most);
-    if (g <= 64) return ops_launch(norm_kernel<T, 64, 1>, quarter, dim3(256), 0, p, stream);
-    if (g <= 128) return ops_launch(norm_kernel<T, 64, 2>, quarter, dim3(256), 0, p, stream);
-    if (g <= 256) return ops_launch(norm_kernel<T, 256, 1>, each, dim3(256), 0, p, stream);
-    if (g <= 512) return ops_launch(norm_kernel<T, 256, 2>, each, dim3(256), 0, p, stream);
-    if (g <= 1024) return ops_launch(norm_kernel<T, 256, 4>, each, dim3(256), 0, p, stream);
-    if (g <= 2048) return ops_launch(norm_kernel<T, 1024, 2>, each, dim3(1024), 0, p, stream);
-    if (g <= 4096) return ops_launch(norm_kernel<T, 1024, 4>, each, dim3(1024), 0, p, stream);
+    if (g <= 64) return ops_launch(norm_kernel<T, true, 1, ONCE>, quarter, dim3(256), 0, p, stream);
+    if (g <= 128) return ops_launch(norm_kernel<T, true, 2, ONCE>, quarter, dim3(256), 0, p, stream);
+    if (g <= 2048) return ops_launch(norm_kernel<T, false, 2, ONCE>, each, dim3((g + 127) / 128 * 64), 0, p, stream);
+    if (g <= 4096) return ops_launch(norm_kernel<T, false, 4, ONCE>, each, dim3(1024), 0, p, stream);
     return ops_launch(norm_long_kernel<T>, each, dim3(1024), 0, p, stream);
 }
 
-template <class T, bool WEIGHTS>
+template <class T, bool WEIGHTS, bool ONCE>
 int launch_norm_back(const NormBackParams &p, u32 grid, void *stream)
 {
     const u32 g = p.groups;
-    if (g <= 64) return ops_launch(norm_back_kernel<T, 64, 1, WEIGHTS>, dim3(grid), dim3(256), 0, p, stream);
-    if (g <= 128) return ops_launch(norm_back_kernel<T, 64, 2, WEIGHTS>, dim3(grid), dim3(256), 0, p, stream);
-    if (g <= 256) return ops_launch(norm_back_kernel<T, 256, 1, WEIGHTS>, dim3(grid), dim3(256), 0, p, stream);
-    if (g <= 512) return ops_launch(norm_back_kernel<T, 256, 2, WEIGHTS>, dim3(grid), dim3(256), 0, p, stream);
-    if (g <= 1024) return ops_launch(norm_back_kernel<T, 512, 2, WEIGHTS>, dim3(grid), dim3(512), 0, p, stream);
-    if (g <= 2048) return ops_launch(norm_back_kernel<T, 1024, 2, WEIGHTS>, dim3(grid), dim3(1024), 0, p, stream);
+    if (g <= 64) return ops_launch(norm_back_kernel<T, true, 1, WEIGHTS, ONCE>, dim3(grid), dim3(256), 0, p, stream);
+    if (g <= 1024) return ops_launch(norm_back_kernel<T, false, 1, WEIGHTS, ONCE>, dim3(grid), dim3((g + 63) / 64 * 64), 0, p, stream);
+    if (g <= 2048) return ops_launch(norm_back_kernel<T, false, 2, WEIGHTS, ONCE>, dim3(grid), dim3((g + 127) / 128 * 64), 0, p, stream);
     return ops_launch(norm_back_long_kernel<T, WEIGHTS>, dim3(grid), dim3(1024), 0, p, stream);
 }
 
 bool wants_weights(const vms_layernorm_backward_args *a) { return a->d_dweight || a->d_dbias; }
 
-// workgroups of the backward pass: as many as are resident at once, each with sums of its own to be joined
+// workgroups of the backward pass: as many as are resident at once (20 wavefronts on a compute unit, 16 of the largest), each
+// with sums of its own to be joined
 u32 back_grid(u64 rows, u64 cols)
 {
-    const u64 groups = (cols + 7) / 8;
-    const u64 blocks = groups <= 128 ? (rows + 3) / 4 : rows;
-    const u64 most = groups <= 512 ? OPS_CUS * 4 : groups <= 1024 ? OPS_CUS * 2 : OPS_CUS;
-    return (u32)(blocks < most ? blocks : most);
+    const u64 groups = (cols + 7) / 8, blocks = groups <= 64 ? (rows + 3) / 4 : rows;
+    const u64 waves = groups <= 64 ? 4 : groups <= 1024 ? (groups + 63) / 64 : 16, each = waves < 20 ? 20 / waves : 1;
+    return (u32)(blocks < OPS_CUS * each ? blocks : OPS_CUS * each);
 }
 
 }  // namespace
@@ -537,7 +551,11 @@ extern "C" int vms_layernorm(const vms_layernorm_args *a, void *stream)
     p.cols = (u32)a->cols;
     p.groups = (p.cols + 7) / 8;
     p.eps = (float)a->eps;
-    return with_type(a->dtype, [&](auto *t) { return launch_norm<std::remove_pointer_t<decltype(t)>>(p, stream); });
+    const bool once = passes_by(a->rows * a->cols * type_bytes(a->dtype) * (2 + (a->d_residual != nullptr) + (a->d_s != nullptr)));
+    return with_type(a->dtype, [&](auto *t) {
+        typedef std::remove_pointer_t<decltype(t)> T;
+        return once ? launch_norm<T, true>(p, stream) : launch_norm<T, false>(p, stream);
+    });
 }
 
 extern "C" size_t vms_layernorm_backward_workspace_bytes(const vms_layernorm_backward_args *a)
@@ -586,7 +604,11 @@ extern "C" int vms_layernorm_backward(const vms_layernorm_backward_args *a, void
     return with_type(a->dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
         if (a->rows) {
-            rc = weights ? launch_norm_back<T, true>(p, grid, stream) : launch_norm_back<T, false>(p, grid, stream);
+            const bool once = passes_by(a->rows * a->cols * type_bytes(a->dtype) * (3 + (a->d_ds != nullptr) + (a->d_dx != nullptr)));
+            if (weights)
+                rc = once ? launch_norm_back<T, true, true>(p, grid, stream) : launch_norm_back<T, true, false>(p, grid, stream);
+            else
+                rc = once ? launch_norm_back<T, false, true>(p, grid, stream) : launch_norm_back<T, false, false>(p, grid, stream);
             if (rc) return rc;
         }
         if (!weights) return (int)VMS_OK;

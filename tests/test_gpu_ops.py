@@ -301,6 +301,19 @@ def test_requests_of_all_tile_sizes_and_more_than_a_wavefront_counts():
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rank", [8, 16, 32, 64, 128])
+def test_short_requests_beside_a_longer_one(rank, dtype):
+    lengths = [1, 2, 1, 0, 3, 1, 1, 9, 1, 1, 1, 2]
+    starts = [2]
+    for n in lengths:
+        starts.append(starts[-1] + n)
+    which = [0, 1, 2, 0, 0, -1, 2, 1, 1, 0, 5, 2]
+    check_low_rank(starts[-1] + 1, 300, 333, rank, dtype, 3, starts, which, scale=[1.0, 0.5, -2.0], step=rank == 16)
+    check_low_rank(2, 64, 1000, rank, dtype, flat=True, step=False)
+    check_low_rank(starts[-1] + 1, 300, 333, rank, dtype, 3, starts, which, inplace=True, step=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
 def test_long_batches(dtype):
     check_low_rank(4100, 512, 768, 16, dtype, flat=True)
     check_low_rank(2100, 256, 384, 64, dtype, 2, [0, 1000, 1003, 2090], [1, 0, 1])
