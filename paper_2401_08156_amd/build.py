@@ -1,12 +1,15 @@
 """Compile the HIP library for gfx950 in-tree (hipcc cross-compiles without a GPU)."""
 import os
 import subprocess
+import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libvmsreplay.so")
+EXT = os.path.join(_HERE, "_vms_torch.so")       # the operators' autograd nodes (host code), linked against LIB
+EXT_SOURCE = "vms_torch_ops.cpp"
 SOURCES = ["vms_replay.hip", "vms_demo.hip", "vms_live.hip", "vms_peaks.hip"]
 OPS_SOURCES = ["vms_dropout.hip", "vms_norm.hip", "vms_lowrank.hip"]
 HEADERS = ["ops_common.hpp", "../../include/vms_ops.h", "wave_hw.hpp", "wave_ops.hpp", "replay_plan.hpp", "replay_kernels.hpp", "replay_fine.hpp", "selftest.hpp", "../../include/vms_replay.h", "../../include/vms_live.h"]
@@ -33,15 +36,15 @@ OPS_FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-shared", "-fPIC", "
 
 
 def _stale():
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(EXT):
         return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, s) for s in SOURCES + OPS_SOURCES + HEADERS]
+    t = min(os.path.getmtime(LIB), os.path.getmtime(EXT))
+    deps = [os.path.join(CSRC, s) for s in SOURCES + OPS_SOURCES + [EXT_SOURCE] + HEADERS]
     return any(os.path.exists(d) and os.path.getmtime(d) > t for d in deps)
 
 
 def build(force=False, save_temps_dir=None):
-    """Build libvmsreplay.so next to this file; returns its path."""
+    """Build libvmsreplay.so and _vms_torch.so next to this file; returns the library's path."""
     if not force and not _stale():
         return LIB
     jobs = [(s, flags) for group, flags in ((SOURCES, HIPCC_FLAGS), (OPS_SOURCES, OPS_FLAGS)) for s in group]
@@ -53,13 +56,32 @@ def build(force=False, save_temps_dir=None):
             obj = os.path.join(objects, source + ".o")
             cmd = ["hipcc"] + [f for f in flags if f != "-shared"] + ["-c", os.path.join(CSRC, source), "-o", obj]
             return obj, _run(cmd + ["--save-temps"] * bool(save_temps_dir), save_temps_dir or CSRC)
+        ext = os.path.join(objects, EXT_SOURCE + ".o")
         with ThreadPoolExecutor(4) as pool:
-            done = list(pool.map(compile_one, jobs))
+            node = pool.submit(_run, _ext_command() + ["-c", os.path.join(CSRC, EXT_SOURCE), "-o", ext], CSRC)
+            done = list(pool.map(compile_one, jobs)) + [(None, node.result())]
         out = "\n".join(text for _, text in done if text.strip())
+        done.pop()
         _run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + [obj for obj, _ in done], CSRC)
+        _run(["g++", "-shared", "-o", EXT, ext, "-L" + _torch_dir("lib"), "-L" + _HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"]
+             + ["-l" + l for l in ("c10", "c10_hip", "torch", "torch_cpu", "torch_python")], CSRC)
     if out:
         print(out)
     return LIB
+
+
+def _torch_dir(*parts):
+    import torch
+    return os.path.join(os.path.dirname(torch.__file__), *parts)
+
+
+def _ext_command():
+    """g++ with PyTorch's headers; HIP's own ask for the platform's name when another compiler reads them."""
+    import torch
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1", "-DTORCH_API_INCLUDE_EXTENSION_H",
+            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+            "-isystem", _torch_dir("include"), "-isystem", _torch_dir("include", "torch", "csrc", "api", "include"),
+            "-isystem", sysconfig.get_paths()["include"], "-isystem", "/opt/rocm/include"]
 
 
 def _run(cmd, cwd):

@@ -75,6 +75,43 @@ def test_recomputation_changes_no_bit(pair):
     assert runs[0] == runs[1]
 
 
+@pytest.mark.parametrize("strategy", torch_plugin.STRATEGIES)
+def test_a_step_frees_what_it_made(strategy):
+    from torch.utils.checkpoint import checkpoint
+    layer, x = make(strategy), torch.randn(70, 96, device="cuda", requires_grad=True)
+
+    def step():
+        h = x
+        for n in range(3):
+            args = (h, layer, n, 0.1, 5)
+            h = checkpoint(torch_plugin.block, *args, use_reentrant=False) if "R" in strategy else torch_plugin.block(*args)
+        torch.autograd.grad(h.sum(), x)
+    step()
+    held = torch.cuda.memory_allocated()
+    for _ in range(4):
+        step()
+    assert torch.cuda.memory_allocated() == held
+
+
+def test_gradients_of_gradients_are_refused():
+    x = torch.randn(8, 16, device="cuda", requires_grad=True)
+    w = torch.ones(16, device="cuda", requires_grad=True)
+    a, b = torch.randn(4, 16, device="cuda", requires_grad=True), torch.randn(16, 4, device="cuda", requires_grad=True)
+    for y in (ops.dropout(x, 0.5, 1), ops.layer_norm(x, w), ops.low_rank_add(x * 1.0, x, a, b)):
+        g, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="first order"):
+            torch.autograd.grad(g.sum(), x)
+
+
+def test_a_sum_changed_in_place_before_the_backward_pass_is_noticed():
+    x, r = [torch.randn(8, 16, device="cuda", requires_grad=True) for _ in range(2)]
+    y, s = ops.layer_norm(x, residual=r)
+    with torch.no_grad():
+        s.add_(1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+
+
 def test_the_strategies_train_and_refuse():
     for s in torch_plugin.STRATEGIES:
         times, loss = torch_plugin.train(2, 64, 2, strategy=s, dropout=0.1, rank=8)
