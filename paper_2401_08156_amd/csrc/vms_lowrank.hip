@@ -45,8 +45,12 @@ struct Some {
     typedef T type __attribute__((ext_vector_type(N)));
     typedef type loose __attribute__((aligned(sizeof(T))));
 };
-template <int N, class T>
-DI typename Some<T, N>::type load_some(const T *p) { return *reinterpret_cast<const typename Some<T, N>::loose *>(p); }
+template <int N, bool ONCE = false, class T>
+DI typename Some<T, N>::type load_some(const T *p)
+{
+    const auto *const from = reinterpret_cast<const typename Some<T, N>::loose *>(p);
+    return ONCE ? __builtin_nontemporal_load(from) : *from;
+}
 // the same, 0 beyond the first n (n may be negative, p is then not followed)
 template <int N, class T>
 DI typename Some<T, N>::type load_first(const T *p, int n)
@@ -483,7 +487,7 @@ DI u32 panel_place(u32 n, u32 ch)
 // Tiles of WR x MR x 16 rows.  A wavefront makes 256 bytes of each of its MR x 16 rows at a time, `trips` times.  WR = 4:
 // the four of them have rows of their own and the same columns, whose part of w they share; WR = 1: the same rows, and
 // columns and panels of their own.
-template <class T, int MR, int JS, int WR>
+template <class T, int MR, int JS, int WR, bool ONCE>
 __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
 {
     typedef typename Mma<T>::Frag Frag;
@@ -560,7 +564,7 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
 #pragma unroll
                 for (int i = 0; i < MR; i++)
 #pragma unroll
-                    for (int u = 0; u < 4; u++) y[i][u] = load_some<EPL>((const T *)(base + yat[i][u]) + c);
+                    for (int u = 0; u < 4; u++) y[i][u] = load_some<EPL, ONCE>((const T *)(base + yat[i][u]) + c);
             }
         } else {
 #pragma unroll
@@ -630,7 +634,11 @@ acc[i][q] = mma(b, h[0][i][s], acc[i][q]);
                 if (row >= rows) continue;
                 T *const dst = (T *)(out + row * (u32)p.ldo * (u32)sizeof(T)) + c;
                 if (LIKELY(n >= EPL)) {
-                    *reinterpret_cast<typename Some<T, EPL>::loose *>(dst) = y[i][u];
+                    auto *const to16 = reinterpret_cast<typename Some<T, EPL>::loose *>(dst);
+                    if (ONCE)
+                        __builtin_nontemporal_store(y[i][u], to16);
+                    else
+                        *to16 = y[i][u];
                 } else {
 #pragma unroll
                     for (int e = 0; e < EPL; e++)
@@ -723,24 +731,28 @@ struct FoldParams {
 };
 
 template <class T>
-__global__ __launch_bounds__(256) void lowrank_fold_kernel(const FoldParams p)
+__global__ __launch_bounds__(64) void lowrank_fold_kernel(const FoldParams p)
 {
     const Hidden &h = p.h[blockIdx.z];
     const bool up = p.up[blockIdx.z], outer = p.outer[blockIdx.z];
     const u32 quads = h.padded / 4;             // four values of four rows a lane
-    const u32 at = blockIdx.x * 256 + threadIdx.x, col = at % quads * 4, row = at / quads * 4;
+    const u32 at = blockIdx.x * 64 + threadIdx.x, col = at % quads * 4, row = at / quads * 4;
     if (row >= p.rows || !(up || outer)) return;
     f32x4 v[4];
 #pragma unroll
     for (int r = 0; r < 4; r++) v[r] = f32x4{ 0.f, 0.f, 0.f, 0.f };
-    for (u32 u = 0; u < h.splits; u++)
+    for (u32 u = 0; u < h.splits; u += 4) {         // four parts' loads under way at a time
+        f32x4 f[4][4];
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+#pragma unroll
+            for (int r = 0; r < 4; r++)
+                f[k][r] = u + k < h.splits && row + r < p.rows ? *(const f32x4 *)(h.parts + ((u64)(u + k) * p.rows + row + r) * h.padded + col) : f32x4{};
 #pragma unroll
         for (int r = 0; r < 4; r++)
-            if (row + r < p.rows) {
-                const f32x4 f = *(const f32x4 *)(h.parts + ((u64)u * p.rows + row + r) * h.padded + col);
 #pragma unroll
-                for (int e = 0; e < 4; e++) v[r][e] += f[e];
-            }
+            for (int e = 0; e < 4; e++) v[r][e] += (f[0][r][e] + f[1][r][e]) + (f[2][r][e] + f[3][r][e]);
+    }
     typedef typename Some<T, 4>::type Four;
 #pragma unroll
     for (int r = 0; r < 4; r++) {
@@ -765,6 +777,8 @@ __global__ __launch_bounds__(256) void lowrank_fold_kernel(const FoldParams p)
     }
 }
 
+// (The last rows' chunks come first: the kernel before has read dout from front to back, and its end may still be in the last
+// cache.)
 struct OuterJob {
     const void *v, *hidden;
     float *sums;
@@ -885,7 +899,7 @@ __global__ __launch_bounds__(256) void lowrank_outer_kernel(const OuterParams p)
     __shared__ float part[4][CQ][64 * 4];
     const u32 blocks = p.job[0].panels * p.job[0].chunks, second = blockIdx.x >= blocks;
     const OuterJob &o = p.job[second];
-    const u32 block = blockIdx.x - (second ? blocks : 0), panel = block % o.panels, chunk = block / o.panels, adapter = blockIdx.y;
+    const u32 block = blockIdx.x - (second ? blocks : 0), panel = block % o.panels, chunk = o.chunks - 1 - block / o.panels, adapter = blockIdx.y;
     const u32 lane = lane_id(), wave = wave_of_group();
     const u32 col = (panel * 16 + (lane & 15)) * CQ;
     const int cols = (int)o.cols - (int)col;
@@ -1059,6 +1073,7 @@ u32 tile_of(const vms_lowrank_args *a)
 
 struct Cut {
     u32 tile16, tiles, splits;  // tile16 8: the kernel with shared weights
+    bool folded;                // the parts are put together before they are read
 };
 
 Cut cut_of(const vms_lowrank_args *a, u64 in)
@@ -1069,12 +1084,14 @@ Cut cut_of(const vms_lowrank_args *a, u64 in)
     c.tile16 = shared ? 8 : tile_of(a);
     const u64 tiles = tiles_of(a, c.tile16), slabs = in * type_bytes(a->dtype) / SLAB_BYTES;
     c.tiles = tiles ? (u32)tiles : 1;
-    // A workgroup for each compute unit, but a slab at least for a wavefront.  Where parts are put together before they are
-    // read it pays to fill all compute units; where `up` reads them, again for each of its panels, only if there are few.
+    // A workgroup for each compute unit, but a slab at least for a wavefront.  Parts that `up` reads, again for each of its
+    // panels, pay only with few tiles.  The kernel with shared weights, of few large tiles, always puts its parts together;
+    // for the others that does not pay (2560 rows of 8192 in 32 bits, 160 tiles: 29 us whole, 31 and 5 in two parts).
     const u64 most = slabs / (shared ? 2 : DOWN_WAVES);
     u64 s = shared || c.tiles < OPS_CUS / 4 ? (OPS_CUS + c.tiles - 1) / c.tiles : 1;
     if (s > most) s = most;
     if (s > (shared ? 8 : 16)) s = shared ? 8 : 16;
+    c.folded = s > 1 && shared;
     c.splits = s ? (u32)s : 1;
     return c;
 }
@@ -1085,16 +1102,15 @@ u32 planes_of(const vms_lowrank_args *a) { return a->dtype != VMS_F32 && a->rows
 size_t laid_out(const vms_lowrank_args *a) { return (a->rows + 15) / 16 * 16 * padded_rank(a->rank) * type_bytes(a->dtype) * planes_of(a); }
 
 size_t parts_bytes(const vms_lowrank_args *a, const Cut &c) { return c.splits > 1 ? (size_t)c.splits * a->rows * padded_rank(a->rank) * 4 : 0; }
-bool folded(const Cut &c) { return c.splits > 1 && c.tile16 == 8; }
 
-size_t hidden_bytes(const vms_lowrank_args *a, const Cut &c) { return (c.splits == 1 || folded(c) ? 2 * laid_out(a) : 0) + parts_bytes(a, c); }
+size_t hidden_bytes(const vms_lowrank_args *a, const Cut &c) { return (c.splits == 1 || c.folded ? 2 * laid_out(a) : 0) + parts_bytes(a, c); }
 
 Hidden hidden_at(const vms_lowrank_args *a, const Cut &c, void *at)
 {
     const u32 padded = padded_rank(a->rank), planes = planes_of(a);
     char *const p = (char *)at;
     if (c.splits == 1) return Hidden{ p, p + laid_out(a), nullptr, 1, padded, planes, false };
-    if (folded(c)) return Hidden{ p, p + laid_out(a), (float *)(p + 2 * laid_out(a)), c.splits, padded, planes, true };
+    if (c.folded) return Hidden{ p, p + laid_out(a), (float *)(p + 2 * laid_out(a)), c.splits, padded, planes, true };
     return Hidden{ nullptr, nullptr, (float *)p, c.splits, padded, planes, false };
 }
 
@@ -1144,7 +1160,7 @@ template <class T>
 int fold(const FoldParams &p, void *stream)
 {
     const u32 lanes = (p.rows + 3) / 4 * (p.h[0].padded / 4);
-    return ops_launch(lowrank_fold_kernel<T>, dim3((lanes + 255) / 256, 1, 2), dim3(256), 0, p, stream);
+    return ops_launch(lowrank_fold_kernel<T>, dim3((lanes + 63) / 64, 1, 2), dim3(64), 0, p, stream);
 }
 
 // The hidden values, whole or in parts that `up` reads; in the order that the products over `in` leave them.
@@ -1155,12 +1171,13 @@ int down(const vms_lowrank_args *a, const Cut &c, const void *x, u64 ldx, const 
     const dim3 grid(c.tiles, c.splits), block(512);
     int rc;
     switch (c.tile16) {
-    case 1: return launch_down<T, 1>(p, c.tiles, stream);
-    case 2: return launch_down<T, 2>(p, c.tiles, stream);
-    case 4: return launch_down<T, 4>(p, c.tiles, stream);
+    case 1: rc = launch_down<T, 1>(p, c.tiles, stream); break;
+    case 2: rc = launch_down<T, 2>(p, c.tiles, stream); break;
+    case 4: rc = launch_down<T, 4>(p, c.tiles, stream); break;
+    default:
+        rc = h->padded == 64 ? ops_launch(lowrank_down_shared_kernel<T, 4>, grid, block, 0, p, stream)
+                             : ops_launch(lowrank_down_shared_kernel<T, 8>, grid, block, 0, p, stream);
     }
-    rc = h->padded == 64 ? ops_launch(lowrank_down_shared_kernel<T, 4>, grid, block, 0, p, stream)
-                         : ops_launch(lowrank_down_shared_kernel<T, 8>, grid, block, 0, p, stream);
     if (rc || !h->folded) return rc;
     const FoldParams f = { { *h, *h }, { true, false }, { true, false }, (u32)a->rows };
     rc = fold<T>(f, stream);
@@ -1168,17 +1185,17 @@ int down(const vms_lowrank_args *a, const Cut &c, const void *x, u64 ldx, const 
     return rc;
 }
 
-template <class T, int MR, int WR>
+template <class T, int MR, int WR, bool ONCE = false>
 int launch_up(const UpParams &p, u32 grid, void *stream)
 {
     const dim3 block(256);
     const int per = Mma<T>::STEP;
     switch (p.h.padded) {
-    case 16: return ops_launch(lowrank_up_kernel<T, MR, 1, WR>, dim3(grid), block, 0, p, stream);
-    case 32: return ops_launch(lowrank_up_kernel<T, MR, 32 / per, WR>, dim3(grid), block, 0, p, stream);
-    case 64: return ops_launch(lowrank_up_kernel<T, MR, 64 / per, WR>, dim3(grid), block, 0, p, stream);
+    case 16: return ops_launch(lowrank_up_kernel<T, MR, 1, WR, ONCE>, dim3(grid), block, 0, p, stream);
+    case 32: return ops_launch(lowrank_up_kernel<T, MR, 32 / per, WR, ONCE>, dim3(grid), block, 0, p, stream);
+    case 64: return ops_launch(lowrank_up_kernel<T, MR, 64 / per, WR, ONCE>, dim3(grid), block, 0, p, stream);
     }
-    return ops_launch(lowrank_up_kernel<T, 1, 128 / per, WR>, dim3(grid), block, 0, p, stream);
+    return ops_launch(lowrank_up_kernel<T, 1, 128 / per, WR, ONCE>, dim3(grid), block, 0, p, stream);
 }
 
 template <class T>
@@ -1207,7 +1224,7 @@ int up(const vms_lowrank_args *a, const Hidden &h, const void *w, const void *ba
         const u64 tiles = a->d_starts ? a->rows / FEW_ROWS + requests + 2 : (a->rows + FEW_ROWS - 1) / FEW_ROWS;
         return up_few<T>(a, h, w, base, ldb, out, ldo, cols, (u32)(tiles < a->rows ? tiles : a->rows), stream);
     }
-    const u32 tile16 = each >= 512 && a->rank <= 64 ? 8 : each >= 48 ? 4 : 1, tiles = (u32)tiles_of(a, tile16);
+    const u32 tile16 = each >= 512 && a->rank <= 64 && base ? 8 : each >= 48 ? 4 : 1, tiles = (u32)tiles_of(a, tile16);
     const u64 trip = (tile16 == 1 ? 4 : 1) * SLAB_BYTES / sizeof(T), all = (cols + trip - 1) / trip;
     // Workgroups enough for four on every compute unit before one takes a second trip; no more than that where each has to
     // find its request first (24 requests, 6007 rows, 4096 -> 4096, rank 32: 22 us, 25 with as many again).
@@ -1219,7 +1236,7 @@ int up(const vms_lowrank_args *a, const Hidden &h, const void *w, const void *ba
     case 1: return launch_up<T, 1, 1>(p, grid, stream);
     case 4: return launch_up<T, 1, 4>(p, grid, stream);
     }
-    return launch_up<T, 2, 4>(p, grid, stream);
+    return passes_by(a->rows * cols * sizeof(T) * (base ? 2 : 1)) ? launch_up<T, 2, 4, true>(p, grid, stream) : launch_up<T, 2, 4>(p, grid, stream);
 }
 
 // columns that a lane takes in the outer products: as many as the registers hold beside the rank
@@ -1302,8 +1319,9 @@ int backward(const vms_lowrank_backward_args *a, void *stream)
         rc = ops_launch(lowrank_swap_kernel<T>, dim3(s.job[0].blocks + s.job[1].blocks, f.n_adapters), dim3(256), 0, s, stream);
         if (!rc) rc = down<T>(&f, l.back, a->d_dout, a->lddout, ws + l.bt, f.out, &dh, stream);
     }
-    if (!rc && a->d_dx) rc = up<T>(&f, dh, ws + l.at, nullptr, 0, a->d_dx, a->lddx, f.in, stream);
-    if (rc || !(a->d_da || a->d_db)) return rc;
+    const auto dx = [&] { return a->d_dx ? up<T>(&f, dh, ws + l.at, nullptr, 0, a->d_dx, a->lddx, f.in, stream) : VMS_OK; };
+    if (rc) return rc;
+    if (!(a->d_da || a->d_db)) return dx();
     FoldParams some = { { h, dh }, {}, { a->d_db && h.parts, a->d_da && dh.parts }, (u32)f.rows };
     if (some.outer[0]) h.outer = some.h[0].outer = ws + l.hfold;
     if (some.outer[1]) dh.outer = some.h[1].outer = ws + l.dfold;
@@ -1311,22 +1329,23 @@ int backward(const vms_lowrank_backward_args *a, void *stream)
         rc = fold<T>(some, stream);
         if (rc) return rc;
     }
-    OuterParams o = { { l.da, l.db }, requests_of(&f), h.planes };
-    o.job[0].v = f.d_x;
-    o.job[0].ldv = f.ldx;
-    o.job[0].hidden = dh.outer;
-    o.job[0].sums = (float *)(ws + l.dasums);
-    o.job[1].v = a->d_dout;
-    o.job[1].ldv = a->lddout;
-    o.job[1].hidden = h.outer;
-    o.job[1].sums = (float *)(ws + l.dbsums);
-    JoinParams j = { { { o.job[0].sums, a->d_da, (u32)f.in, l.da.chunks, 0 }, { o.job[1].sums, a->d_db, (u32)f.out, l.db.chunks, 1 } },
-                     f.rank, padded, (u32)((f.in + 255) / 256) };
-    u32 blocks = (u32)((f.out + 255) / 256);
-    if (!a->d_da) o.job[0].chunks = j.first_blocks = 0;
-    if (!a->d_db) o.job[1].chunks = blocks = 0;
+    OuterParams o = { { l.db, l.da }, requests_of(&f), h.planes };
+    o.job[0].v = a->d_dout;
+    o.job[0].ldv = a->lddout;
+    o.job[0].hidden = h.outer;
+    o.job[0].sums = (float *)(ws + l.dbsums);
+    o.job[1].v = f.d_x;
+    o.job[1].ldv = f.ldx;
+    o.job[1].hidden = dh.outer;
+    o.job[1].sums = (float *)(ws + l.dasums);
+    JoinParams j = { { { o.job[0].sums, a->d_db, (u32)f.out, l.db.chunks, 1 }, { o.job[1].sums, a->d_da, (u32)f.in, l.da.chunks, 0 } },
+                     f.rank, padded, (u32)((f.out + 255) / 256) };
+    u32 blocks = (u32)((f.in + 255) / 256);
+    if (!a->d_db) o.job[0].chunks = j.first_blocks = 0;
+    if (!a->d_da) o.job[1].chunks = blocks = 0;
     const u32 grid = o.job[0].panels * o.job[0].chunks + o.job[1].panels * o.job[1].chunks;
     rc = launch_outer<T>(o, padded, dim3(grid, f.n_adapters), stream);
+    if (!rc) rc = dx();
     if (rc) return rc;
     return ops_launch(lowrank_join_kernel<T>, dim3(j.first_blocks + blocks, (f.rank + 7) / 8, f.n_adapters), dim3(256), 0, j, stream);
 }
