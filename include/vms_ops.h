@@ -74,7 +74,7 @@ int vms_dropout(const vms_dropout_args *a, void *stream);
 typedef struct vms_layernorm_args {
     uint32_t struct_size;        /* sizeof(vms_layernorm_args)                                      */
     uint32_t dtype;
-    uint64_t rows, cols;         /* each below 2^31, cols >= 1                                      */
+    uint64_t rows, cols;         /* rows below 2^31, cols from 1 to 2^26 - 1                        */
     const void *d_x, *d_residual, *d_weight, *d_bias;
     void *d_y, *d_s;
     float *d_stats;
@@ -125,7 +125,7 @@ typedef struct vms_lowrank_args {
     uint64_t rows, in, out;      /* rows < 2^28, in and out in 1 .. 2^22 - 1                        */
     uint32_t rank;               /* 1 .. VMS_LOWRANK_MAX_RANK                                       */
     uint32_t n_adapters;         /* 1 .. 65535                                                      */
-    uint32_t n_requests;         /* < 2^22; ignored if d_starts is NULL                             */
+    uint32_t n_requests;         /* < 2^16; ignored if d_starts is NULL                             */
     float scale;                 /* used if d_scales is NULL                                        */
     const float *d_scales;       /* nullable: one for each adapter                                  */
     const void *d_x, *d_y, *d_a, *d_b;      /* a and b without gaps                                 */

@@ -1120,12 +1120,46 @@ int check(const vms_lowrank_args *a)
     if (a->struct_size != sizeof *a) return VMS_ESTRUCT;
     if (a->dtype > VMS_BF16 || a->rows >> 28 || !a->in || a->in >> 22 || !a->out || a->out >> 22) return VMS_EINVAL;
     if (!a->rank || a->rank > VMS_LOWRANK_MAX_RANK || !a->n_adapters || a->n_adapters > 65535) return VMS_EINVAL;
-    if (a->d_starts && a->n_requests >> 22) return VMS_EINVAL;
+    if (a->d_starts && a->n_requests >> 16) return VMS_EINVAL;       // (every workgroup looks through them)
     return VMS_OK;
 }
 
 // places inside a tile of 128 rows are counted in 32 bits
 bool near_ok(u64 ld) { return ld < 1u << 23; }
+
+// How `up` cuts a batch: tiles of 16 * tile16 rows (0: FEW_ROWS, the kernel for single tokens), panels of `trips` trips.
+struct UpCut {
+    u32 tile16, tiles, trips, panels;
+    u64 groups;             // workgroups
+};
+
+UpCut up_cut(const vms_lowrank_args *a, u64 cols, bool base)
+{
+    UpCut c;
+    const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
+    const u32 epl = 16 / type_bytes(a->dtype), chunks = a->rank / epl;
+    const bool few = each <= 2 && a->rank % epl == 0 && chunks <= 16 && (chunks & (chunks - 1)) == 0;
+    c.tile16 = few ? 0 : each >= 512 && a->rank <= 64 && base ? 8 : each >= 48 ? 4 : 1;
+    u64 tiles = tiles_of(a, few ? 1 : c.tile16);
+    if (few) {
+        tiles = a->d_starts ? a->rows / FEW_ROWS + requests + 2 : (a->rows + FEW_ROWS - 1) / FEW_ROWS;
+        if (tiles > a->rows) tiles = a->rows;
+    }
+    c.tiles = (u32)tiles;
+    const u64 trip = few ? 256 : (c.tile16 == 1 ? 4 : 1) * (SLAB_BYTES / type_bytes(a->dtype)), all = (cols + trip - 1) / trip;
+    // Workgroups enough for four on every compute unit before one takes a second trip; no more than that where each has to
+    // find its request first (24 requests, 6007 rows, 4096 -> 4096, rank 32: 22 us, 25 with as many again; one token each of
+    // 96 requests, 4096 -> 16384, rank 16: 12 us, 16 with three times as many).
+    u64 trips = (all * tiles + (a->d_starts || few ? OPS_CUS * 4 - 1 : 0)) / (OPS_CUS * 4);
+    trips = trips < 1 ? 1 : trips > 8 ? 8 : trips;
+    c.trips = (u32)trips;
+    c.panels = (u32)((all + trips - 1) / trips);
+    c.groups = tiles * c.panels;
+    return c;
+}
+
+// a launch has fewer than 2^32 lanes (`down` has fewer workgroups than that for any batch, and these for any that memory holds)
+bool grid_ok(const UpCut &c) { return c.groups < 1u << 24; }
 
 int check_inputs(const vms_lowrank_args *a)
 {
@@ -1199,44 +1233,25 @@ int launch_up(const UpParams &p, u32 grid, void *stream)
 }
 
 template <class T>
-int up_few(const vms_lowrank_args *a, const Hidden &h, const void *w, const void *base, u64 ldb, void *out, u64 ldo, u64 cols, u32 tiles, void *stream)
-{
-    const u64 all = (cols + 255) / 256;
-    u64 trips = (all * tiles + OPS_CUS * 4 - 1) / (OPS_CUS * 4);
-    trips = trips > 8 ? 8 : trips;
-    const UpParams p = { h, w, base, out, requests_of(a), ldb, ldo, (u32)cols, a->rank, (u32)trips, (u32)((all + trips - 1) / trips) };
-    const dim3 grid(tiles * p.panels), block(256);
-    switch (a->rank / Mma<T>::EPL) {
-    case 1: return ops_launch(lowrank_up_few_kernel<T, 1>, grid, block, 0, p, stream);
-    case 2: return ops_launch(lowrank_up_few_kernel<T, 2>, grid, block, 0, p, stream);
-    case 4: return ops_launch(lowrank_up_few_kernel<T, 4>, grid, block, 0, p, stream);
-    case 8: return ops_launch(lowrank_up_few_kernel<T, 8>, grid, block, 0, p, stream);
-    }
-    return ops_launch(lowrank_up_few_kernel<T, 16>, grid, block, 0, p, stream);
-}
-
-template <class T>
 int up(const vms_lowrank_args *a, const Hidden &h, const void *w, const void *base, u64 ldb, void *out, u64 ldo, u64 cols, void *stream)
 {
-    const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
-    const u32 chunks = a->rank / Mma<T>::EPL;
-    if (each <= 2 && a->rank % Mma<T>::EPL == 0 && chunks <= 16 && (chunks & (chunks - 1)) == 0) {
-        const u64 tiles = a->d_starts ? a->rows / FEW_ROWS + requests + 2 : (a->rows + FEW_ROWS - 1) / FEW_ROWS;
-        return up_few<T>(a, h, w, base, ldb, out, ldo, cols, (u32)(tiles < a->rows ? tiles : a->rows), stream);
-    }
-    const u32 tile16 = each >= 512 && a->rank <= 64 && base ? 8 : each >= 48 ? 4 : 1, tiles = (u32)tiles_of(a, tile16);
-    const u64 trip = (tile16 == 1 ? 4 : 1) * SLAB_BYTES / sizeof(T), all = (cols + trip - 1) / trip;
-    // Workgroups enough for four on every compute unit before one takes a second trip; no more than that where each has to
-    // find its request first (24 requests, 6007 rows, 4096 -> 4096, rank 32: 22 us, 25 with as many again).
-    u64 trips = (all * tiles + (a->d_starts ? OPS_CUS * 4 - 1 : 0)) / (OPS_CUS * 4);
-    trips = trips < 1 ? 1 : trips > 8 ? 8 : trips;
-    const UpParams p = { h, w, base, out, requests_of(a), ldb, ldo, (u32)cols, a->rank, (u32)trips, (u32)((all + trips - 1) / trips) };
-    const u32 grid = tiles * p.panels;
-    switch (tile16) {
+    const UpCut c = up_cut(a, cols, base != nullptr);
+    const UpParams p = { h, w, base, out, requests_of(a), ldb, ldo, (u32)cols, a->rank, c.trips, c.panels };
+    const u32 grid = (u32)c.groups;
+    const bool once = passes_by(a->rows * cols * sizeof(T) * (base ? 2 : 1));
+    switch (c.tile16) {
     case 1: return launch_up<T, 1, 1>(p, grid, stream);
-    case 4: return launch_up<T, 1, 4>(p, grid, stream);
+    case 4: return once ? launch_up<T, 1, 4, true>(p, grid, stream) : launch_up<T, 1, 4>(p, grid, stream);
+    case 8: return once ? launch_up<T, 2, 4, true>(p, grid, stream) : launch_up<T, 2, 4>(p, grid, stream);
     }
-    return passes_by(a->rows * cols * sizeof(T) * (base ? 2 : 1)) ? launch_up<T, 2, 4, true>(p, grid, stream) : launch_up<T, 2, 4>(p, grid, stream);
+    const dim3 blocks(grid), block(256);
+    switch (a->rank / Mma<T>::EPL) {
+    case 1: return ops_launch(lowrank_up_few_kernel<T, 1>, blocks, block, 0, p, stream);
+    case 2: return ops_launch(lowrank_up_few_kernel<T, 2>, blocks, block, 0, p, stream);
+    case 4: return ops_launch(lowrank_up_few_kernel<T, 4>, blocks, block, 0, p, stream);
+    case 8: return ops_launch(lowrank_up_few_kernel<T, 8>, blocks, block, 0, p, stream);
+    }
+    return ops_launch(lowrank_up_few_kernel<T, 16>, blocks, block, 0, p, stream);
 }
 
 // columns that a lane takes in the outer products: as many as the registers hold beside the rank
@@ -1378,6 +1393,7 @@ extern "C" int vms_lowrank(const vms_lowrank_args *a, void *stream)
     if (rc) return rc;
     if (!input_ok(a->d_y, a->dtype) || !near_ok(a->ldy) || !output_ok(a->d_out, a->dtype, a->ldo, a->out) || !near_ok(a->ldo)) return VMS_EINVAL;
     if (a->d_y == a->d_out && a->ldy != a->ldo) return VMS_EINVAL;
+    if (!grid_ok(up_cut(a, a->out, true))) return VMS_EINVAL;
     const Cut c = cut_of(a, a->in);
     Hidden h = hidden_at(a, c, a->d_hidden);
     return with_type(a->dtype, [&](auto *t) {
@@ -1413,6 +1429,7 @@ extern "C" int vms_lowrank_backward(const vms_lowrank_backward_args *a, void *st
     if (!input_ok(a->d_dout, f.dtype) || !near_ok(a->lddout)) return VMS_EINVAL;
     if (a->d_dx && (!output_ok(a->d_dx, f.dtype, a->lddx, f.in) || !near_ok(a->lddx))) return VMS_EINVAL;
     if (!a->d_dx && !a->d_da && !a->d_db) return VMS_OK;
+    if (a->d_dx && !grid_ok(up_cut(&f, f.in, false))) return VMS_EINVAL;
     if (!a->d_workspace || (uintptr_t)a->d_workspace % 16 || a->workspace_bytes < layout_of(a).total) return VMS_EWORKSPACE;
     return with_type(f.dtype, [&](auto *t) { return backward<std::remove_pointer_t<decltype(t)>>(a, stream); });
 }

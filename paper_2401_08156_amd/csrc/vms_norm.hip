@@ -529,7 +529,7 @@ extern "C" int vms_layernorm(const vms_layernorm_args *a, void *stream)
     NormParams p;
     int rc = make_mask(a->mask, &p.mask);
     if (rc) return rc;
-    if (a->dtype > VMS_BF16 || a->rows >> 31 || a->cols >> 31 || !a->cols || !(a->eps >= 0.0)) return VMS_EINVAL;
+    if (a->dtype > VMS_BF16 || a->rows >> 31 || a->cols >> 26 || !a->cols || !(a->eps >= 0.0)) return VMS_EINVAL;
     if (!a->rows) return VMS_OK;
     if (!input_ok(a->d_x, a->dtype) || !output_ok(a->d_y, a->dtype, a->ldy, a->cols)) return VMS_EINVAL;
     if (a->d_residual ? !input_ok(a->d_residual, a->dtype) : a->mask.p > 0.0 || a->d_s) return VMS_EINVAL;
@@ -561,7 +561,7 @@ extern "C" int vms_layernorm(const vms_layernorm_args *a, void *stream)
 
 extern "C" size_t vms_layernorm_backward_workspace_bytes(const vms_layernorm_backward_args *a)
 {
-    if (!a || a->struct_size != sizeof *a || a->rows >> 31 || a->cols >> 31 || !wants_weights(a)) return 0;
+    if (!a || a->struct_size != sizeof *a || a->rows >> 31 || a->cols >> 26 || !wants_weights(a)) return 0;
     return (size_t)back_grid(a->rows, a->cols) * 2 * a->cols * sizeof(float);
 }
 
@@ -572,7 +572,7 @@ extern "C" int vms_layernorm_backward(const vms_layernorm_backward_args *a, void
     NormBackParams p;
     int rc = make_mask(a->mask, &p.mask);
     if (rc) return rc;
-    if (a->dtype > VMS_BF16 || a->rows >> 31 || a->cols >> 31 || !a->cols) return VMS_EINVAL;
+    if (a->dtype > VMS_BF16 || a->rows >> 31 || a->cols >> 26 || !a->cols) return VMS_EINVAL;
     const bool weights = wants_weights(a);
     for (const void *d : { a->d_dweight, a->d_dbias })
         if (d && !input_ok(d, a->dtype)) return VMS_EINVAL;

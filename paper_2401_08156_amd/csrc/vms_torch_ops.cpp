@@ -135,12 +135,13 @@ vms_dropout_mask mask_of(double p, const Seed &s, uint64_t call)
 
 uint64_t word(const py::handle &v, const char *what)
 {
-    const unsigned long long n = PyLong_Check(v.ptr()) ? PyLong_AsUnsignedLongLong(v.ptr()) : (unsigned long long)-1;
-    if (!PyLong_Check(v.ptr()) || (n == (unsigned long long)-1 && PyErr_Occurred())) {
+    const py::object n = py::reinterpret_steal<py::object>(PyNumber_Index(v.ptr()));        // int, numpy's integers
+    const unsigned long long w = n ? PyLong_AsUnsignedLongLong(n.ptr()) : 0;
+    if (PyErr_Occurred()) {
         PyErr_Clear();
         refuse(std::string(what) + " is a number of 64 bits, got " + py::cast<std::string>(py::repr(v)));
     }
-    return n;
+    return w;
 }
 
 Seed seed_of(const py::handle &v, const Tensor &x)

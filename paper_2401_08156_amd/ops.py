@@ -15,7 +15,8 @@ below are those of the C entry points, for programs that call them with pointers
 
 Tensors may have any strides.  Rows (the last dimension) that are not consecutive in memory, or leading dimensions that
 are not evenly spaced, are copied first.  A call can be captured into a graph; what it allocates then belongs to the
-graph.  To replay one with another mask each time, pass `seed` as a tensor and change it between the replays.
+graph.  To replay one with another mask each time, pass `seed` as a tensor and change it between the replays.  As with every
+operator, a backward pass is captured only while no eager graph of the same leaves is alive.
 """
 import ctypes
 import importlib.util
@@ -112,7 +113,7 @@ def dropout(x, p, seed, call=0, residual=None):
 
     Which ones depends on their row (all dimensions but the last, counted through) and column, on `seed` and on `call`
     alone: 64-bit numbers of which a program gives every dropout of a step a `call` of its own and every step another
-    seed.  `seed` may be an int64 tensor of one element on the same device, read when the kernel runs; it must not
+    seed.  `seed` may be an int64 tensor of one element on the same device, whose 64 bits are read when the kernel runs; it must not
     change before the backward pass.  p is taken in steps of 2^-16.  Nothing is kept for the backward pass but `seed`."""
     return (_nodes or nodes()).dropout(x, p, seed, call, residual)
 
@@ -133,7 +134,7 @@ def low_rank_add(y, x, a, b, scale=1.0, starts=None, which=None, inplace=False):
     out, rank], and the rows of x and y packed by request: request i has rows starts[i] to starts[i + 1] - 1 and adapter
     which[i] (none if that is negative), with `starts` and `which` int32 on the device.  `starts` does not decrease; rows
     before starts[0] and from starts[-1] on belong to no request, and their sum is y.  `scale` is a number or a float32
-    tensor with one for each adapter.  Ranks up to 128.
+    tensor with one for each adapter.  Ranks up to 128, requests up to 65535.
 
     `inplace` makes the sum in y itself and leaves rows of no request untouched.  Gradients: of y, x, a and b; an
     adapter's are summed over all its requests.  Kept for the backward pass: x, a, b, and scale * x a^T."""

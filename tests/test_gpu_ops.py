@@ -314,6 +314,59 @@ def test_short_requests_beside_a_longer_one(rank, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rank", [3, 20, 50, 100, 127])
+def test_few_rows_and_every_padded_rank(rank, dtype):
+    check_low_rank(7, 520, 700, rank, dtype, flat=True)
+    check_low_rank(60, 130, 260, rank, dtype, 2, [0, 20, 25, 57], [1, 0, 1])
+
+
+def test_numbers_of_numpy_as_seeds():
+    import numpy as np
+    x, x64 = normal((5, 40), torch.float32, 1)
+    check_dropout(ops.dropout(x, np.float64(0.5), np.int64(3), np.uint32(4)), x64, 0.5, torch.float32, seed=3, call=4)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+def test_outputs_larger_than_the_last_cache(dtype):
+    # (accesses marked as not to be kept) the oracle sees some rows; the sums over all rows are left to the other tests
+    n = 4096 if dtype == torch.float32 else 8192
+    rows = (300 << 20) // (3 * n * (4 if dtype == torch.float32 else 2))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    new = lambda *s: torch.randn(s, generator=g, device="cuda").to(dtype)
+    x, r, dy, ds = [new(rows, n).requires_grad_(i < 2) for i in range(4)]
+    w = new(n).requires_grad_(True)
+    some = torch.tensor([0, 1, rows // 2, rows - 1])
+    kept, factor = oo.mask((rows, n), 0.3, SEED, CALL)
+    x64, r64, dy64, ds64 = [t.detach()[some.cuda()].cpu().double() for t in (x, r, dy, ds)]
+    s64 = r64 + oo.drop(x64, kept[some], factor)
+    y = ops.dropout(x, 0.3, SEED, CALL, residual=r)
+    size = x64.abs() * factor + r64.abs()
+    oo.assert_within("dropout", y[some.cuda()], s64, oo.unit(dtype) * s64.abs() + 2 * oo.E32 * size + oo.tiny(dtype))
+    y, s = ops.layer_norm(x, w, residual=r, p=0.3, seed=SEED, call=CALL)
+    w64 = w.detach().cpu().double()
+    want, _, saved = oo.norm(s64, w64, None, 1e-5)
+    e_y, e_s, _ = oo.norm_bounds(dtype, x64, w64, None, r64, factor, want, s64, saved)
+    oo.assert_within("y", y[some.cuda()], want, e_y)
+    oo.assert_within("s", s[some.cuda()], s64, e_s)
+    dx, dr, dw = torch.autograd.grad([y, s], [x, r, w], [dy, ds])
+    at = s.detach()[some.cuda()].cpu().double()
+    here, _, saved = oo.norm(at, w64, None, 1e-5)
+    e_h = oo.norm_bounds(dtype, at, w64, None, None, 1.0, here, at, saved)[2]
+    h, q = saved
+    g64 = dy64 * w64
+    dr64 = q * (g64 - g64.mean(-1, keepdim=True) - h * (g64 * h).mean(-1, keepdim=True)) + ds64
+    dx64 = oo.drop(dr64, kept[some], factor)
+    bounds = oo.norm_backward_bounds(dtype, dy64, ds64, saved, w64, (dx64, dr64, torch.zeros(n), torch.zeros(n)), e_h, factor)
+    oo.assert_within("dx", dx[some.cuda()], dx64, bounds[0])
+    oo.assert_within("dr", dr[some.cuda()], dr64, bounds[1])
+    a, b = new(40, 64) * 0.1, new(n, 40) * 0.1
+    z = new(rows, 64)
+    out = ops.low_rank_add(x.detach(), z, a, b)
+    want, bound = oo.low_rank(dtype, x64, z[some.cuda()].cpu().double(), a.cpu().double()[None], b.cpu().double()[None], [1.0])["out"]
+    oo.assert_within("out", out[some.cuda()], want, bound)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
 def test_long_batches(dtype):
     check_low_rank(4100, 512, 768, 16, dtype, flat=True)
     check_low_rank(2100, 256, 384, 64, dtype, 2, [0, 1000, 1003, 2090], [1, 0, 1])

@@ -135,7 +135,7 @@ def changed(a, kw):
         (dict(d_x=None), EINVAL), (dict(d_y=None), EINVAL), (dict(d_x=P + 1), EINVAL), (dict(d_residual=P + 1), EINVAL),
         (dict(ldy=15), EINVAL), (dict(ldx=1 << 31), EINVAL)]],
     *[("vms_layernorm", norm_args, kw, code) for kw, code in [
-        (dict(struct_size=8), ESTRUCT), (dict(dtype=9), EINVAL), (dict(cols=0), EINVAL), (dict(rows=1 << 40), EINVAL),
+        (dict(struct_size=8), ESTRUCT), (dict(dtype=9), EINVAL), (dict(cols=0), EINVAL), (dict(cols=1 << 26), EINVAL), (dict(rows=1 << 40), EINVAL),
         (dict(eps=-1.0), EINVAL), (dict(eps=float("nan")), EINVAL), (dict(p=2.0), EINVAL), (dict(d_x=None), EINVAL),
         (dict(d_y=P + 2), EINVAL), (dict(d_residual=None), EINVAL), (dict(d_residual=None, p=0.0), EINVAL),
         (dict(d_weight=P + 2), EINVAL), (dict(d_stats=P + 2), EINVAL), (dict(ldy=8), EINVAL), (dict(lds=8), EINVAL)]],
@@ -147,7 +147,7 @@ def changed(a, kw):
     *[("vms_lowrank", lowrank_args, kw, code) for kw, code in [
         (dict(struct_size=8), ESTRUCT), (dict(dtype=3), EINVAL), (dict(rows=1 << 28), EINVAL), (dict(in_=0), EINVAL),
         (dict(out=1 << 22), EINVAL), (dict(rank=0), EINVAL), (dict(rank=129), EINVAL), (dict(n_adapters=0), EINVAL),
-        (dict(n_adapters=65536), EINVAL), (dict(n_requests=1 << 22), EINVAL), (dict(d_x=None), EINVAL), (dict(d_a=None), EINVAL),
+        (dict(n_adapters=65536), EINVAL), (dict(n_requests=1 << 16), EINVAL), (dict(rows=(1 << 28) - 1, n_requests=1 << 15, out=(1 << 22) - 1, rank=5, ldy=1 << 22, ldo=1 << 22, d_out=2 * P, hidden_bytes=1 << 50), EINVAL), (dict(d_x=None), EINVAL), (dict(d_a=None), EINVAL),
         (dict(d_b=P + 1), EINVAL), (dict(d_y=None), EINVAL), (dict(d_out=None), EINVAL), (dict(ldo=31), EINVAL),
         (dict(d_which=None), EINVAL), (dict(d_starts=P + 2), EINVAL), (dict(ldy=64), EINVAL), (dict(d_hidden=None), EWORKSPACE),
         (dict(d_hidden=P + 4), EWORKSPACE), (dict(hidden_bytes=64), EWORKSPACE)]],
