@@ -156,7 +156,7 @@ DI u32 die_order(u32 b, u32 n)
 const u32 OPS_CUS = 256;        // compute units of the device that the grids are sized for
 
 // Does a call that reads and writes so many bytes leave nothing of them in the last cache (256 MiB)?  Then its accesses are
-// marked as not to be kept: dropout of 4096 x 16384 in 16 bits, 268 MB, takes 46 us, 51 without the marks.  A smaller call's
+// marked as not to be kept: dropout of 4096 x 16384 in 16 bits, 268 MB, takes 48 us, 51 without the marks.  A smaller call's
 // output may be found there by the next kernel.
 inline bool passes_by(u64 bytes) { return bytes > 256u << 20; }
 

@@ -325,10 +325,9 @@ __global__ __launch_bounds__(WAVES * 64) void lowrank_down_kernel(const DownPara
     }
 }
 
-// The same for long requests and ranks above 32.  There the weights, read once for 32 rows, are two thirds of what goes
-// through the vector cache, whose requests in flight are what bounds the kernel above (110 lines a compute unit, 0.98 us each,
-// 2.9 TB/s of x).  Here four wavefronts with 32 rows each share them in the LDS, a slab for each half of the workgroup at a
-// time, and the next slabs are on their way meanwhile.
+// The same for long requests, long sums and ranks above 32.  There the weights, read once for 32 rows, are two thirds of what
+// goes through the vector cache.  Here four wavefronts with 32 rows each share them in the LDS, a slab for each half of the
+// workgroup at a time, and the next slabs are on their way meanwhile.
 template <class T, int NR>
 __global__ __launch_bounds__(512) void lowrank_down_shared_kernel(const DownParams p)
 {
@@ -649,7 +648,8 @@ acc[i][q] = mma(b, h[0][i][s], acc[i][q]);
     }
 }
 
-// The same for requests of one token or two, where all there is to read is w: a lane has 16 bytes of it, the CPR lanes of a
+// The same for requests of one token or two (96 of them, 4096 -> 16384 at rank 16: 12 us, 18 with the matrix units, which have
+// one row in 16 to work on).  All there is to read is w: a lane has 16 bytes of it, the CPR lanes of a
 // column put their sums together, and a wavefront makes 64 columns at a time.  A chunk of the rank belongs to the same lane
 // in all of them, so its part of the (up to ROWS) rows' hidden values stays in registers, in 32 bits.
 const int FEW_ROWS = 4;
@@ -1080,7 +1080,10 @@ Cut cut_of(const vms_lowrank_args *a, u64 in)
 {
     Cut c;
     const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
-    const bool shared = a->rank > 32 && each >= 128 && a->rows >= 2048;
+    // Shared weights save reads from the caches, as many as there are steps and ranks, and cost a launch: 8192 rows at rank 64
+    // take 71 us with them and 82 without over 16384 columns, 26 and 23 over 4096; at rank 128 and 4096 columns the whole
+    // step of 8192 rows 238 and 252 us.
+    const bool shared = a->rank > 32 && in * padded_rank(a->rank) >= 1u << 19 && each >= 128 && a->rows >= 2048;
     c.tile16 = shared ? 8 : tile_of(a);
     const u64 tiles = tiles_of(a, c.tile16), slabs = in * type_bytes(a->dtype) / SLAB_BYTES;
     c.tiles = tiles ? (u32)tiles : 1;

@@ -380,6 +380,14 @@ def test_long_requests_of_high_rank(rank, dtype):
     check_low_rank(2048, 1111, 1300, rank, dtype, flat=True)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+def test_long_sums_of_high_rank(dtype):
+    check_low_rank(2055, 8200, 300, 64, dtype, 2, [5, 900, 1003, 2049], [1, 0, 1])
+    check_low_rank(2048, 300, 8193, 40, dtype, flat=True)
+    check_low_rank(2100, 4101, 200, 128, dtype, flat=True)
+    check_low_rank(2100, 200, 4097, 100, dtype, 2, [0, 130, 2000], [1, 0], scale=[0.5, 2.0])
+
+
 def test_single_tokens_through_wide_layers():
     for rank in (1, 16, 64):
         check_low_rank(1, 8192, 8192, rank, torch.bfloat16, step=False, flat=True)
