@@ -14,6 +14,8 @@
  * tensors of a call; every sum is kept in 32 bits.  rows = 0 is allowed and does nothing
  * but clear the gradients of weights.
  *
+ * Outputs overlap neither each other nor an input, but where an entry point says so.
+ *
  * Pointers named d_* are DEVICE pointers owned by the caller, on the current HIP device.
  * Calls are asynchronous on `stream` (a hipStream_t of that device), allocate nothing,
  * keep nothing and can be captured into a graph.  They return VMS_OK or a negative VMS_E*
@@ -122,7 +124,8 @@ int vms_layernorm_backward(const vms_layernorm_backward_args *a, void *stream);
 typedef struct vms_lowrank_args {
     uint32_t struct_size;        /* sizeof(vms_lowrank_args)                                        */
     uint32_t dtype;
-    uint64_t rows, in, out;      /* rows < 2^28, in and out in 1 .. 2^22 - 1                        */
+    uint64_t rows, in, out;      /* rows < 2^28 (2^27 with ranks above 64), in and out in 1 .. 2^22 - 1;
+                                    refused where a launch cannot have as many workgroups           */
     uint32_t rank;               /* 1 .. VMS_LOWRANK_MAX_RANK                                       */
     uint32_t n_adapters;         /* 1 .. 65535                                                      */
     uint32_t n_requests;         /* < 2^16; ignored if d_starts is NULL                             */

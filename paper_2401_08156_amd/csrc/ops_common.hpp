@@ -165,7 +165,9 @@ int ops_launch(void (*kernel)(P), dim3 grid, dim3 block, u32 lds, const P &p, vo
 {
     P copy = p;
     void *args[] = { &copy };
-    return hipLaunchKernel((const void *)kernel, grid, block, args, lds, (hipStream_t)stream) == hipSuccess ? VMS_OK : VMS_EHIP;
+    if (hipLaunchKernel((const void *)kernel, grid, block, args, lds, (hipStream_t)stream) == hipSuccess) return VMS_OK;
+    (void)hipGetLastError();            // reported here, and not again by whoever asks next
+    return VMS_EHIP;
 }
 
 // calls f with a null pointer of the element type; VMS_EINVAL for a type that does not exist

@@ -609,8 +609,7 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
                 for (int s = 0; s < JS; s++) {
                     const Frag b = to[panel_place<CPR, SLAB / 4>(n, s * (STEP / EPL) + group)];
 #pragma unroll
-                    for (int i = 0; i < MR; i++)
-acc[i][q] = mma(b, h[0][i][s], acc[i][q]);
+                    for (int i = 0; i < MR; i++) acc[i][q] = mma(b, h[0][i][s], acc[i][q]);
                     if (two) {
 #pragma unroll
                         for (int i = 0; i < MR; i++) acc[i][q] = mma(b, h[PLANES - 1][i][s], acc[i][q]);
@@ -1161,8 +1160,9 @@ UpCut up_cut(const vms_lowrank_args *a, u64 cols, bool base)
     return c;
 }
 
-// a launch has fewer than 2^32 lanes (`down` has fewer workgroups than that for any batch, and these for any that memory holds)
+// a launch has fewer than 2^32 lanes: of `up` 256 in a workgroup, of `down` 512 (1024 where tiles are few)
 bool grid_ok(const UpCut &c) { return c.groups < 1u << 24; }
+bool grid_ok(const Cut &c) { return c.tiles < 1u << 23; }
 
 int check_inputs(const vms_lowrank_args *a)
 {
@@ -1398,6 +1398,7 @@ extern "C" int vms_lowrank(const vms_lowrank_args *a, void *stream)
     if (a->d_y == a->d_out && a->ldy != a->ldo) return VMS_EINVAL;
     if (!grid_ok(up_cut(a, a->out, true))) return VMS_EINVAL;
     const Cut c = cut_of(a, a->in);
+    if (!grid_ok(c)) return VMS_EINVAL;
     Hidden h = hidden_at(a, c, a->d_hidden);
     return with_type(a->dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
@@ -1433,6 +1434,7 @@ extern "C" int vms_lowrank_backward(const vms_lowrank_backward_args *a, void *st
     if (a->d_dx && (!output_ok(a->d_dx, f.dtype, a->lddx, f.in) || !near_ok(a->lddx))) return VMS_EINVAL;
     if (!a->d_dx && !a->d_da && !a->d_db) return VMS_OK;
     if (a->d_dx && !grid_ok(up_cut(&f, f.in, false))) return VMS_EINVAL;
+    if (!grid_ok(cut_of(&f, f.out))) return VMS_EINVAL;
     if (!a->d_workspace || (uintptr_t)a->d_workspace % 16 || a->workspace_bytes < layout_of(a).total) return VMS_EWORKSPACE;
     return with_type(f.dtype, [&](auto *t) { return backward<std::remove_pointer_t<decltype(t)>>(a, stream); });
 }

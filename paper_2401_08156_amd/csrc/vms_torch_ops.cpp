@@ -59,14 +59,16 @@ void same(const Tensor &x, std::initializer_list<const Tensor *> others)
                    " beside " + c10::toString(x.scalar_type()) + " on " + x.device().str());
 }
 
-// a tensor as rows of its last dimension; a copy where its strides do not allow that
+// a tensor as rows of its last dimension; a copy where its strides do not allow that, or rows are `far` elements apart
+// (what the library's entry points refuse)
+const uint64_t FAR = 1ull << 31, LOWRANK_FAR = 1ull << 23;
 struct Matrix {
     Tensor t;
     uint64_t ld = 0;
     const void *ptr() const { return t.defined() ? t.const_data_ptr() : nullptr; }
 };
 
-Matrix matrix(const Tensor &t)
+Matrix matrix(const Tensor &t, uint64_t far = FAR)
 {
     if (!t.defined()) return {};
     const int64_t n = t.dim(), cols = t.size(-1);
@@ -82,7 +84,7 @@ Matrix matrix(const Tensor &t)
                 even = false;
             wanted = t.stride(i) * t.size(i);
         }
-        if (even) return { t, (uint64_t)(stride < 0 ? cols : stride) };
+        if (even && (stride < 0 || (uint64_t)stride < far)) return { t, (uint64_t)(stride < 0 ? cols : stride) };
     }
     return { t.contiguous(), (uint64_t)cols };
 }
@@ -350,7 +352,7 @@ vms_lowrank_args lowrank_args(const Matrix &x, const Tensor &a, const Tensor &b,
 // -> y + ..., and what the backward pass reads
 std::pair<Tensor, Tensor> run_low_rank(const Tensor &y, const Tensor &x, const Tensor &a, const Tensor &b, const Batch &batch, bool inplace)
 {
-    const Matrix m = matrix(x), base = matrix(y);
+    const Matrix m = matrix(x, LOWRANK_FAR), base = matrix(y, LOWRANK_FAR);
     vms_lowrank_args f = lowrank_args(m, a, b, batch);
     Tensor out = inplace ? y : like(y);
     f.d_y = base.ptr();
@@ -382,7 +384,7 @@ struct LowRankAdd : torch::autograd::Function<LowRankAdd> {
         Tensor dx, da, db;
         if (need_x || need_a || need_b) {
             const at::NoGradGuard guard;
-            const Matrix m = matrix(x), d = matrix(dout);
+            const Matrix m = matrix(x, LOWRANK_FAR), d = matrix(dout, LOWRANK_FAR);
             if (need_x) dx = like(x);
             if (need_a) da = like(a);
             if (need_b) db = like(b);
@@ -432,14 +434,21 @@ Tensor low_rank_add(const Tensor &y, const Tensor &x, const Tensor &a_, const Te
             refuse("a scale tensor is a contiguous float32 vector with one number for each adapter");
         if (scales.requires_grad()) refuse("scales have no gradient");
     } else {
-        factor = py::cast<double>(scale);
+        factor = PyFloat_AsDouble(scale.ptr());
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            refuse("scale is a number or a tensor, got " + py::cast<std::string>(py::repr(scale)));
+        }
     }
-    if (inplace && !matrix(y).t.is_same(y)) refuse("y's strides do not allow the sum in place");
+    if (inplace && !matrix(y, LOWRANK_FAR).t.is_same(y)) refuse("y's strides do not allow the sum in place");
+    if (inplace && at::GradMode::is_enabled() && y.requires_grad() && y.is_leaf()) refuse("the sum in place of a leaf that requires a gradient");
     const py::gil_scoped_release go;
     const Tensor a = a_.contiguous(), b = b_.contiguous();
     const Batch batch = { factor, scales, starts, which };
     if (wanted({ &y, &x, &a, &b })) return LowRankAdd::apply(y, x, a, b, batch, inplace);
-    return run_low_rank(y, x, a, b, batch, inplace).first;
+    const Tensor out = run_low_rank(y, x, a, b, batch, inplace).first;
+    if (inplace) y.unsafeGetTensorImpl()->bump_version();       // as a node's mark_dirty does: what was saved of y is noticed
+    return out;
 }
 
 }  // namespace

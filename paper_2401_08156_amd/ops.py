@@ -13,8 +13,8 @@ The kernels of libvmsreplay.so do all the work, called from the autograd nodes o
 wrong arguments raise ValueError or VmsError, and there is no other path for tensors that are not on a GPU.  The structures
 below are those of the C entry points, for programs that call them with pointers of their own.
 
-Tensors may have any strides.  Rows (the last dimension) that are not consecutive in memory, or leading dimensions that
-are not evenly spaced, are copied first.  A call can be captured into a graph; what it allocates then belongs to the
+Tensors may have any strides.  Rows (the last dimension) that are not consecutive in memory, leading dimensions that are not
+evenly spaced, and rows 2^31 elements apart (2^23 for adapters) are copied first.  A call can be captured into a graph; what it allocates then belongs to the
 graph.  To replay one with another mask each time, pass `seed` as a tensor and change it between the replays.  As with every
 operator, a backward pass is captured only while no eager graph of the same leaves is alive.
 """

@@ -401,6 +401,29 @@ def test_low_rank_strides(dtype):
     check_low_rank(40, 40, 40, 8, dtype, cut=lambda t: t.t())
 
 
+def test_adapters_on_rows_far_apart():
+    """As the last tokens of long sequences are: the rows of x, y and dout 2^23 elements apart and a little more"""
+    far = lambda t: torch.zeros(3, (1 << 23) + 8, dtype=t.dtype, device="cuda")[:, -64:].copy_(t) if t.is_cuda else t
+    check_low_rank(3, 64, 64, 8, torch.bfloat16, cut=far)
+    z = torch.zeros(3, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="in place"):
+        ops.low_rank_add(far(z), z, z.new_zeros(8, 64), z.new_zeros(64, 8), inplace=True)
+
+
+def test_a_sum_in_place_is_noticed_by_what_was_saved():
+    x, a, b = torch.randn(5, 64, device="cuda"), torch.randn(8, 64, device="cuda"), torch.randn(64, 8, device="cuda")
+    leaf = torch.randn(5, 64, device="cuda", requires_grad=True)
+    y = torch.tanh(leaf)
+    with torch.no_grad():
+        assert ops.low_rank_add(y, x, a, b, inplace=True) is y
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    before = leaf.detach().clone()
+    with pytest.raises(ValueError, match="leaf"):
+        ops.low_rank_add(leaf, x, a, b, inplace=True)
+    assert torch.equal(leaf.detach(), before)
+
+
 @pytest.mark.parametrize("starts,which", [(None, None), ([2, 9, 30], [1, -1]), ([0, 35], [0])])
 def test_the_sum_in_place_leaves_other_rows_alone(starts, which):
     check_low_rank(40, 64, 72, 8, torch.bfloat16, 1 if starts is None else 2, starts, which, inplace=True)
@@ -505,6 +528,7 @@ def test_refusals():
         lambda: ops.low_rank_add(z(3, 4), z(3, 5), z(2, 5), z(4, 2), scale=z(2)),
         lambda: ops.low_rank_add(z(3, 4), z(3, 5), z(2, 5), z(4, 2), scale=z(1).half()),
         lambda: ops.low_rank_add(z(3, 4), z(3, 5), z(2, 5), z(4, 2), scale=z(1).requires_grad_(True)),
+        lambda: ops.low_rank_add(z(3, 4), z(3, 5), z(2, 5), z(4, 2), scale="2"),
         lambda: ops.low_rank_add(z(4, 3).t(), z(3, 5), z(2, 5), z(4, 2), inplace=True),
     ]
     for n, call in enumerate(bad):

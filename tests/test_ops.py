@@ -150,11 +150,14 @@ def changed(a, kw):
         (dict(n_adapters=65536), EINVAL), (dict(n_requests=1 << 16), EINVAL), (dict(rows=(1 << 28) - 1, n_requests=1 << 15, out=(1 << 22) - 1, rank=5, ldy=1 << 22, ldo=1 << 22, d_out=2 * P, hidden_bytes=1 << 50), EINVAL), (dict(d_x=None), EINVAL), (dict(d_a=None), EINVAL),
         (dict(d_b=P + 1), EINVAL), (dict(d_y=None), EINVAL), (dict(d_out=None), EINVAL), (dict(ldo=31), EINVAL),
         (dict(d_which=None), EINVAL), (dict(d_starts=P + 2), EINVAL), (dict(ldy=64), EINVAL), (dict(d_hidden=None), EWORKSPACE),
-        (dict(d_hidden=P + 4), EWORKSPACE), (dict(hidden_bytes=64), EWORKSPACE)]],
+        (dict(d_hidden=P + 4), EWORKSPACE), (dict(hidden_bytes=64), EWORKSPACE),
+        # (more workgroups than a launch can have, of either product)
+        (dict(rows=1 << 27, rank=128, n_requests=1, d_out=2 * P, hidden_bytes=1 << 50), EINVAL)]],
     *[("vms_lowrank_backward", lowrank_backward_args, kw, code) for kw, code in [
         (dict(struct_size=8), ESTRUCT), (dict(f=dict(struct_size=8)), ESTRUCT), (dict(f=dict(rank=200)), EINVAL),
         (dict(f=dict(d_x=None)), EINVAL), (dict(f=dict(d_hidden=None)), EWORKSPACE), (dict(d_dout=None), EINVAL),
-        (dict(d_da=P + 1), EINVAL), (dict(lddx=63), EINVAL), (dict(d_workspace=None), EWORKSPACE), (dict(workspace_bytes=100), EWORKSPACE)]],
+        (dict(d_da=P + 1), EINVAL), (dict(lddx=63), EINVAL), (dict(d_workspace=None), EWORKSPACE), (dict(workspace_bytes=100), EWORKSPACE),
+        (dict(f=dict(rows=1 << 27, rank=128, n_requests=1, hidden_bytes=1 << 50), workspace_bytes=1 << 50), EINVAL)]],
 ])
 def test_the_c_entry_points_refuse(name, make, kw, code):
     assert getattr(ops.lib(), name)(ctypes.byref(make(**kw)), None) == code
@@ -234,6 +237,14 @@ def test_rows_of_any_strides(make, same, stride):
     rows = t.numel() // cols
     flat = torch.as_strided(m, (rows, cols), (ld, 1), m.storage_offset())
     assert torch.equal(flat, t.reshape(rows, cols)) and flat.shape == t.reshape(rows, cols).shape
+
+
+def test_rows_too_far_apart_for_the_library_are_copied():
+    for apart, same in (((1 << 31) - 1, True), (1 << 31, False)):
+        t = torch.empty(apart + 8, dtype=torch.int8).as_strided((2, 8), (apart, 1))     # (memory that nothing touches is not taken)
+        t[0], t[1] = torch.arange(8), torch.arange(8, 16)
+        m, ld = ops.nodes().matrix(t)
+        assert (m is t) == same and ld == (apart if same else 8) and torch.equal(m, torch.arange(16, dtype=torch.int8).reshape(2, 8))
 
 
 @pytest.mark.parametrize("module,argv", [
