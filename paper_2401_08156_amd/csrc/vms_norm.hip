@@ -61,18 +61,18 @@ DI void norm_input(const NormParams &p, u64 seed, u32 row, u32 group, float v[8]
     }
 }
 
+// y, and s where it is wanted, of eight columns; w and b: those of weight and bias
 template <class T, bool ONCE>
-DI void norm_output(const NormParams &p, u32 row, u32 group, const float v[8], float mean, float rstd)
+DI void norm_output(const NormParams &p, u32 row, u32 group, const float v[8], const typename Eight<T>::type &w, const typename Eight<T>::type &b,
+                    float mean, float rstd)
 {
     const u32 col = group * 8, n = p.cols - col;
-    float w[8], b[8], o[8];
-    if (p.weight) load8((const T *)p.weight + col, n, w);
-    if (p.bias) load8((const T *)p.bias + col, n, b);
+    float o[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         o[i] = (v[i] - mean) * rstd;
-        if (p.weight) o[i] *= w[i];
-        if (p.bias) o[i] += b[i];
+        if (p.weight) o[i] *= (float)w[i];
+        if (p.bias) o[i] += (float)b[i];
     }
     store8<ONCE>((T *)p.y + row * p.ldy + col, n, o);
     if (p.s) store8<ONCE>((T *)p.s + row * p.lds + col, n, v);
@@ -138,23 +138,53 @@ __global__ __launch_bounds__(SINGLE ? 256 : 1024) void norm_kernel(const NormPar
         n[g] = p.cols > col ? p.cols - col : 0;
         mine += p.cols > at ? min(p.cols - at, 512u) : 0u;
     }
+    typedef typename Eight<T>::type Raw;
     for (u32 row = SINGLE ? blockIdx.x * 4 + wave : blockIdx.x; row < p.rows; row += step) {
+        // What the row needs is on its way before the first of it is waited for, the weights too where registers hold them
+        // (4099 x 5120 in 16 bits: 28 us, 32 with each load waited for before the next).
+        const bool AHEAD = NG < 4, WEIGHTS_AHEAD = AHEAD && NG * sizeof(T) <= 8;
+        Raw x[NG], r[NG], w[NG], b[NG];
+        const auto fetch = [&](int g) {
+            const u32 col = (g * lanes + lane) * 8;
+            x[g] = r[g] = Raw{};
+            if (!n[g]) return;
+            x[g] = load8_raw<ONCE>((const T *)p.x + row * p.ldx + col, n[g]);
+            if (p.residual) r[g] = load8_raw<ONCE>((const T *)p.residual + row * p.ldr + col, n[g]);
+        };
+        const auto fetch_weights = [&](int g) {
+            const u32 col = (g * lanes + lane) * 8;
+            w[g] = b[g] = Raw{};
+            if (!n[g]) return;
+            if (p.weight) w[g] = load8_raw((const T *)p.weight + col, n[g]);
+            if (p.bias) b[g] = load8_raw((const T *)p.bias + col, n[g]);
+        };
+#pragma unroll
+        for (int g = 0; g < NG; g++)
+            if (AHEAD) fetch(g);
+#pragma unroll
+        for (int g = 0; g < NG; g++)
+            if (WEIGHTS_AHEAD) fetch_weights(g);
         float v[NG][8];
 #pragma unroll
         for (int g = 0; g < NG; g++) {
+            if (!AHEAD) fetch(g);
 #pragma unroll
-            for (int i = 0; i < 8; i++) v[g][i] = 0.f;
-            if (n[g]) norm_input<T, ONCE>(p, seed, row, g * lanes + lane, v[g]);
+            for (int i = 0; i < 8; i++) v[g][i] = (float)x[g][i];
+            if (p.mask.limit) drop8(p.mask, seed, row, g * lanes + lane, v[g]);
+            if (p.residual) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) v[g][i] += (float)r[g][i];
+            }
         }
         float sum, m2, sum2 = 0.f, m22 = 0.f;
         part_stats<NG>(v, n, mine, &sum, &m2);
         if (rounded) {
-            float r[NG][8];
+            float as_stored[NG][8];
 #pragma unroll
             for (int g = 0; g < NG; g++)
 #pragma unroll
-                for (int i = 0; i < 8; i++) r[g][i] = (float)(T)v[g][i];
-            part_stats<NG>(r, n, mine, &sum2, &m22);
+                for (int i = 0; i < 8; i++) as_stored[g][i] = (float)(T)v[g][i];
+            part_stats<NG>(as_stored, n, mine, &sum2, &m22);
         }
         float count = (float)mine;
         if (SINGLE) {               // one part
@@ -193,8 +223,10 @@ __global__ __launch_bounds__(SINGLE ? 256 : 1024) void norm_kernel(const NormPar
             }
         }
 #pragma unroll
-        for (int g = 0; g < NG; g++)
-            if (n[g]) norm_output<T, ONCE>(p, row, g * lanes + lane, v[g], mean, rstd);
+        for (int g = 0; g < NG; g++) {
+            if (!WEIGHTS_AHEAD) fetch_weights(g);
+            if (n[g]) norm_output<T, ONCE>(p, row, g * lanes + lane, v[g], w[g], b[g], mean, rstd);
+        }
     }
 }
 
@@ -235,8 +267,12 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const NormParams p)
             p.stats[(u64)row * 2 + 1] = 1.f / sqrtf(m2[rounded] + p.eps);
         }
         for (u32 group = threadIdx.x; group < p.groups; group += 1024) {
+            const u32 col = group * 8, n = p.cols - col;
+            typename Eight<T>::type w = {}, b = {};
+            if (p.weight) w = load8_raw((const T *)p.weight + col, n);
+            if (p.bias) b = load8_raw((const T *)p.bias + col, n);
             norm_input<T, false>(p, seed, row, group, v);
-            norm_output<T, false>(p, row, group, v, mean[0], rstd);
+            norm_output<T, false>(p, row, group, v, w, b, mean[0], rstd);
         }
     }
 }
@@ -483,17 +519,26 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const NormJoinParams p)
     }
 }
 
-// Which registers hold a row: those of a wavefront up to 1024 columns, those of a workgroup of as many wavefronts as it needs
-// up to 16384 (two groups a lane; to 32768 with four), none beyond.  A workgroup for each row: many of them at different stages
-// keep the memory busier than ones that stay and read a row ahead, of which fewer fit (122 and 131 us for 16384 x 4096 in 16 bits).
+// Which registers hold a row.  Those of one wavefront up to 512 columns (1024 in 16 bits, two groups a lane), those of a
+// workgroup beyond, none above 32768.  More than four wavefronts are a multiple of four, for the four units that they are
+// spread over.  A lane takes one group up to 2048 columns (6144 in 32 bits), then two or three, as leaves fewer lanes without
+// any: 4099 rows of 5120 columns in 16 bits take 24 us with four wavefronts of three groups a lane, 28 with five of two; in 32
+// bits 42 with twelve of one, 45 with ten.
+// A workgroup for each row: many of them at different stages keep the memory busier than ones that stay and read a row ahead,
+// of which fewer fit (122 and 131 us for 16384 x 4096 in 16 bits with residual and dropout).
 template <class T, bool ONCE>
 int launch_norm(const NormParams &p, void *stream)
 {
     const u32 g = p.groups, most = 1u << 18;      // workgroups; they go on to further rows
     const dim3 quarter(p.rows / 4 < most ? (p.rows + 3) / 4 : most), each(p.rows < most ? p.rows : most);
+    const auto fours = [g](u32 groups) { return (g + 256 * groups - 1) / (256 * groups) * 4; };      // wavefronts
+    const dim3 one((g <= 256 ? (g + 63) / 64 : fours(1)) * 64), two(fours(2) * 64), three(fours(3) * 64);
     if (g <= 64) return ops_launch(norm_kernel<T, true, 1, ONCE>, quarter, dim3(256), 0, p, stream);
-    if (g <= 128) return ops_launch(norm_kernel<T, true, 2, ONCE>, quarter, dim3(256), 0, p, stream);
-    if (g <= 2048) return ops_launch(norm_kernel<T, false, 2, ONCE>, each, dim3((g + 127) / 128 * 64), 0, p, stream);
+    if constexpr (sizeof(T) == 2)
+        if (g <= 128) return ops_launch(norm_kernel<T, true, 2, ONCE>, quarter, dim3(256), 0, p, stream);
+    if (g <= (sizeof(T) == 2 ? 256 : 768)) return ops_launch(norm_kernel<T, false, 1, ONCE>, each, one, 0, p, stream);
+    if (two.x <= 1024 && two.x * 2 <= three.x * 3) return ops_launch(norm_kernel<T, false, 2, ONCE>, each, two, 0, p, stream);
+    if (three.x <= 1024) return ops_launch(norm_kernel<T, false, 3, ONCE>, each, three, 0, p, stream);
     if (g <= 4096) return ops_launch(norm_kernel<T, false, 4, ONCE>, each, dim3(1024), 0, p, stream);
     return ops_launch(norm_long_kernel<T>, each, dim3(1024), 0, p, stream);
 }
@@ -510,13 +555,13 @@ int launch_norm_back(const NormBackParams &p, u32 grid, void *stream)
 
 bool wants_weights(const vms_layernorm_backward_args *a) { return a->d_dweight || a->d_dbias; }
 
-// Workgroups of the backward pass: 16 wavefronts on a compute unit, each workgroup with sums of its own to be joined.  All are
-// resident at once; 20, which the registers would hold, make the pass no faster and the join slower (4099 x 5120 in 16 bits:
-// 44 us with 16, 48 with 20, 50 with 30).
-u32 back_grid(u64 rows, u64 cols)
+// Workgroups of the backward pass, each with sums of its own to be joined: 16 wavefronts on a compute unit, 8 in 32 bits, whose
+// loads are twice as large (4099 x 5120 in 16 bits: 42 us with 10 wavefronts, 46 with 20, 53 with 40; 2816 x 2048 in 32 bits
+// 21 with 8, 22 with 16).
+u32 back_grid(u32 dtype, u64 rows, u64 cols)
 {
     const u64 groups = (cols + 7) / 8, blocks = groups <= 64 ? (rows + 3) / 4 : rows;
-    const u64 waves = groups <= 64 ? 4 : groups <= 1024 ? (groups + 63) / 64 : 16, each = waves < 16 ? 16 / waves : 1;
+    const u64 waves = groups <= 64 ? 4 : groups <= 1024 ? (groups + 63) / 64 : 16, resident = dtype == VMS_F32 ? 8 : 16, each = waves < resident ? resident / waves : 1;
     return (u32)(blocks < OPS_CUS * each ? blocks : OPS_CUS * each);
 }
 
@@ -562,7 +607,7 @@ extern "C" int vms_layernorm(const vms_layernorm_args *a, void *stream)
 extern "C" size_t vms_layernorm_backward_workspace_bytes(const vms_layernorm_backward_args *a)
 {
     if (!a || a->struct_size != sizeof *a || a->rows >> 31 || a->cols >> 26 || !wants_weights(a)) return 0;
-    return (size_t)back_grid(a->rows, a->cols) * 2 * a->cols * sizeof(float);
+    return (size_t)back_grid(a->dtype, a->rows, a->cols) * 2 * a->cols * sizeof(float);
 }
 
 extern "C" int vms_layernorm_backward(const vms_layernorm_backward_args *a, void *stream)
@@ -601,7 +646,7 @@ extern "C" int vms_layernorm_backward(const vms_layernorm_backward_args *a, void
     p.rows = (u32)a->rows;
     p.cols = (u32)a->cols;
     p.groups = (p.cols + 7) / 8;
-    const u32 grid = back_grid(a->rows, a->cols);
+    const u32 grid = back_grid(a->dtype, a->rows, a->cols);
     return with_type(a->dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
         if (a->rows) {
