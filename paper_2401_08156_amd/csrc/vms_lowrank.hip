@@ -8,7 +8,7 @@
 //   outer   da = dhidden^T x, db = dout^T hidden, summed over rows: a lane reads some columns of eight rows and swaps
 //                                    them in its own registers
 // The forward pass is down and up; the backward pass is down on dout with b transposed, up with a transposed, and outer
-// twice.  The order of the summed elements is the same for both operands of a product, so any order will do.
+// twice.  Single tokens of small adapters have a forward pass of one launch (`one`).  The order of the summed elements is the same for both operands of a product, so any order will do.
 //
 // The operands want a row in each of 16 neighbouring lanes, the memory path 64 consecutive bytes in each four: taken as the
 // operands want them, loads of 16 bytes a lane go through the address unit one lane at a time (64 accesses an instruction by
@@ -268,15 +268,13 @@ DI void down_slab(const char *x, const char *w, const u32 (&xat)[MR][4], const u
     }
 }
 
-// MR x 16 rows and the whole rank in a workgroup; its WAVES wavefronts, and `splits` workgroups, share the summed dimension.
-template <class T, int MR, int NR, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void lowrank_down_kernel(const DownParams p)
+// A wavefront's share of the sums for a tile's MR x 16 rows and the whole rank: a slab in `shares`, and for the last one what
+// is left of a row.  Tiles begin at different places (`turn`): rows are often a power of two apart, so that what all tiles read
+// at one place is in one channel of the caches.
+template <class T, int MR, int NR>
+DI void down_sums(const DownParams &p, const Tile &t, u32 share, u32 shares, u32 turn, f32x4 (&acc)[MR][NR])
 {
-    const u32 SLAB = SLAB_BYTES / sizeof(T);
-    __shared__ f32x4 part[WAVES][NR][64];
-    Tile t;
-    if (!find_tile<MR * 16>(p.q, blockIdx.x, &t) || t.adapter < 0) return;
-    const u32 lane = lane_id(), wave = wave_of_group();
+    const u32 SLAB = SLAB_BYTES / sizeof(T), lane = lane_id();
     const char *const x = (const char *)((const T *)p.x + t.row * p.ldx);
     const char *const w = (const char *)((const T *)p.w + (u64)t.adapter * p.rank * p.in);
     u32 xat[MR][4], wat[NR][4];     // rows beyond the tile and the rank are the last one again: their results go nowhere
@@ -287,23 +285,30 @@ __global__ __launch_bounds__(WAVES * 64) void lowrank_down_kernel(const DownPara
 #pragma unroll
         for (int j = 0; j < NR; j++) wat[j][u] = min(j * 16 + slab_row(lane, u), p.rank - 1) * p.in * (u32)sizeof(T) + slab_byte(lane);
     }
-    f32x4 acc[MR][NR];
 #pragma unroll
     for (int i = 0; i < MR; i++)
 #pragma unroll
         for (int j = 0; j < NR; j++) acc[i][j] = f32x4{ 0.f, 0.f, 0.f, 0.f };
-
-    // A wavefront takes a slab and leaves the next ones to the others.  Tiles begin at different places: rows are often a
-    // power of two apart, so that what all tiles read at one place is in one channel of the caches.
-    const u32 slabs = p.in / SLAB, shares = p.h.splits * WAVES, share = blockIdx.y * WAVES + wave;
-    const u32 turn = slabs ? blockIdx.x * WAVES % slabs : 0;
+    const u32 slabs = p.in / SLAB;
+    turn = slabs ? turn % slabs : 0;
     for (u32 s = share; s < slabs; s += shares) {
         const u64 at = (u64)(s + turn < slabs ? s + turn : s + turn - slabs) * SLAB_BYTES;
         down_slab<T, MR, NR, true>(x + at, w + at, xat, wat, 0, acc);
     }
     if (share == shares - 1 && slabs * SLAB < p.in)
         down_slab<T, MR, NR, false>(x + (u64)slabs * SLAB_BYTES, w + (u64)slabs * SLAB_BYTES, xat, wat, (int)(p.in - slabs * SLAB), acc);
+}
 
+// MR x 16 rows and the whole rank in a workgroup; its WAVES wavefronts, and `splits` workgroups, share the summed dimension.
+template <class T, int MR, int NR, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void lowrank_down_kernel(const DownParams p)
+{
+    __shared__ f32x4 part[WAVES][NR][64];
+    Tile t;
+    if (!find_tile<MR * 16>(p.q, blockIdx.x, &t) || t.adapter < 0) return;
+    const u32 lane = lane_id(), wave = wave_of_group();
+    f32x4 acc[MR][NR];
+    down_sums<T, MR, NR>(p, t, blockIdx.y * WAVES + wave, p.h.splits * WAVES, blockIdx.x * WAVES, acc);
     const float scale = p.scales ? p.scales[t.adapter] : p.scale;
 #pragma unroll
     for (int i = 0; i < MR; i++) {
@@ -648,10 +653,60 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
 }
 
 // The same for requests of one token or two (96 of them, 4096 -> 16384 at rank 16: 12 us, 18 with the matrix units, which have
-// one row in 16 to work on).  All there is to read is w: a lane has 16 bytes of it, the CPR lanes of a
-// column put their sums together, and a wavefront makes 64 columns at a time.  A chunk of the rank belongs to the same lane
-// in all of them, so its part of the (up to ROWS) rows' hidden values stays in registers, in 32 bits.
+// one row in 16 to work on), where the forward pass is not the one launch below, and for their dx.  All there is to read is w:
+// a lane has 16 bytes of it, the CPR lanes of a column put their sums together, and a wavefront makes 64 columns at a time.  A
+// chunk of the rank belongs to the same lane in all of them, so its part of the (up to FEW_ROWS) rows' hidden values stays in
+// registers, in 32 bits.
 const int FEW_ROWS = 4;
+
+// What 64 columns need: w, and the column of base that a lane keeps
+template <class T, int CPR>
+struct Few {
+    typename Mma<T>::Frag w[CPR];
+    T y[FEW_ROWS];
+};
+
+template <int CPR>
+DI u32 few_column(u32 c0) { return c0 + lane_id() % CPR * (64 / CPR) + lane_id() / CPR; }
+
+template <class T, int CPR>
+DI void few_load(const UpParams &p, const Tile &t, u32 c0, Few<T, CPR> &f)
+{
+    const int EPL = Mma<T>::EPL;
+    const u32 lane = lane_id(), col = few_column<CPR>(c0);
+    const T *const w = (const T *)p.w + (u64)max(t.adapter, 0) * p.cols * p.rank;
+#pragma unroll
+    for (int i = 0; i < CPR; i++) f.w[i] = load_some<EPL>(w + (u64)min(c0 + (i * 64 + lane) / CPR, p.cols - 1) * p.rank + lane % CPR * EPL);
+#pragma unroll
+    for (int r = 0; r < FEW_ROWS; r++) {
+        f.y[r] = (T)0.f;
+        if (p.base && (u32)r < t.rows && col < p.cols) f.y[r] = ((const T *)p.base)[(t.row + r) * p.ldb + col];
+    }
+}
+
+template <class T, int CPR>
+DI void few_store(const UpParams &p, const Tile &t, u32 c0, const Few<T, CPR> &f, const float (&h)[FEW_ROWS][Mma<T>::EPL])
+{
+    const u32 chunk = lane_id() % CPR, col = few_column<CPR>(c0);
+#pragma unroll
+    for (int r = 0; r < FEW_ROWS; r++) {
+        if ((u32)r >= t.rows) break;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < CPR; i++) {
+            float v = 0.f;
+#pragma unroll
+            for (int e = 0; e < Mma<T>::EPL; e++) v += h[r][e] * (float)f.w[i][e];
+            if (CPR > 1) v = dpp_add<DPP_QUAD_XOR1, 0xF>(v);
+            if (CPR > 2) v = dpp_add<DPP_QUAD_XOR2, 0xF>(v);
+            if (CPR > 4) v = dpp_add<DPP_ROW_HALF_MIRROR, 0xF>(v);
+            if (CPR > 8) v = dpp_add<DPP_ROW_MIRROR, 0xF>(v);
+            sum = chunk == i ? v : sum;
+        }
+        const float y = (float)f.y[r];
+        if (col < p.cols) ((T *)p.out)[(t.row + r) * p.ldo + col] = (T)(t.adapter < 0 ? y : y + sum);
+    }
+}
 
 template <class T, int CPR>
 __global__ __launch_bounds__(256) void lowrank_up_few_kernel(const UpParams p)
@@ -685,38 +740,73 @@ __global__ __launch_bounds__(256) void lowrank_up_few_kernel(const UpParams p)
             }
         }
     }
-    const T *const w = (const T *)p.w + (u64)(none ? 0 : t.adapter) * p.cols * p.rank;
     u32 c0 = (block % p.panels * p.trips * 4 + wave_of_group()) * 64;
     for (u32 trip = 0; trip < p.trips && c0 < p.cols; trip++, c0 += 256) {
-        Frag b[CPR];
+        Few<T, CPR> f;
+        few_load(p, t, c0, f);
+        few_store(p, t, c0, f, h);
+    }
+}
+
+// Both products in one launch, for few tokens of small adapters: every workgroup makes the hidden values of its tile itself,
+// which costs it the read of a and saves the wait for another kernel.  The weights of the first columns, and then always those
+// of the next, are on their way meanwhile.
+const int ONE_WAVES = 8;
+
+struct OneParams {
+    DownParams d;
+    UpParams u;
+};
+
+template <class T, int CPR>
+__global__ __launch_bounds__(ONE_WAVES * 64) void lowrank_one_kernel(const OneParams p)
+{
+    const int EPL = Mma<T>::EPL, NR = CPR * EPL > 16 ? CPR * EPL / 16 : 1;
+    const bool NEXT = CPR <= 4;     // (the registers of the others do not hold two)
+    __shared__ f32x4 part[ONE_WAVES][NR][64];
+    __shared__ float hidden[FEW_ROWS][NR * 16];
+    Tile t;
+    const u32 block = die_order(blockIdx.x, gridDim.x), panel = block % p.u.panels, rank = p.d.rank;
+    if (!find_tile<FEW_ROWS>(p.d.q, block / p.u.panels, &t)) return;
+    const bool none = t.adapter < 0;
+    if (none && p.u.base == p.u.out) return;
+    const u32 lane = lane_id(), wave = wave_of_group(), step = ONE_WAVES * 64;
+    u32 c0 = (panel * p.u.trips * ONE_WAVES + wave) * 64;
+    const u32 upto = min((panel + 1) * p.u.trips * step, p.u.cols);
+    Few<T, CPR> f[NEXT ? 2 : 1];
+    if (NEXT && c0 < upto) few_load(p.u, t, c0, f[0]);
+    float h[FEW_ROWS][EPL] = {};
+    if (!none) {
+        f32x4 acc[1][NR];
+        down_sums<T, 1, NR>(p.d, t, wave, ONE_WAVES, block * ONE_WAVES, acc);
 #pragma unroll
-        for (int i = 0; i < CPR; i++) {
-            const u32 col = c0 + (i * 64 + lane) / CPR;
-            b[i] = load_some<EPL>(w + (u64)min(col, p.cols - 1) * p.rank + chunk * EPL);
+        for (int j = 0; j < NR; j++) part[wave][j][lane] = acc[0][j];
+        __syncthreads();
+        const float scale = p.d.scales ? p.d.scales[t.adapter] : p.d.scale;
+        for (u32 at = threadIdx.x; at < NR * 64; at += step) {
+            const u32 j = at >> 6, l = at & 63, row = l & 15, col = j * 16 + (l >> 4) * 4;
+            f32x4 v = part[0][j][l];
+#pragma unroll
+            for (int u = 1; u < ONE_WAVES; u++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) v[e] += part[u][j][l][e];
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[e] = col + e < rank ? v[e] * scale : 0.f;
+            if (row >= t.rows) continue;
+            *(f32x4 *)&hidden[row][col] = v;
+            if (panel == 0) store_hidden<T>(p.d.h, v, t.row + row, col, 0, p.d.q.rows);      // for the backward pass
         }
-        const u32 col = c0 + chunk * (64 / CPR) + lane / CPR;        // the one that this lane keeps
-        float y[FEW_ROWS], sum[FEW_ROWS];
+        __syncthreads();
 #pragma unroll
-        for (int r = 0; r < FEW_ROWS; r++) {
-            y[r] = sum[r] = 0.f;
-            if (p.base && (u32)r < t.rows && col < p.cols) y[r] = (float)((const T *)p.base)[(t.row + r) * p.ldb + col];
-        }
+        for (int r = 0; r < FEW_ROWS; r++)
 #pragma unroll
-        for (int r = 0; r < FEW_ROWS; r++) {
-            if ((u32)r >= t.rows) break;
-#pragma unroll
-            for (int i = 0; i < CPR; i++) {
-                float v = 0.f;
-#pragma unroll
-                for (int e = 0; e < EPL; e++) v += h[r][e] * (float)b[i][e];
-                if (CPR > 1) v = dpp_add<DPP_QUAD_XOR1, 0xF>(v);
-                if (CPR > 2) v = dpp_add<DPP_QUAD_XOR2, 0xF>(v);
-                if (CPR > 4) v = dpp_add<DPP_ROW_HALF_MIRROR, 0xF>(v);
-                if (CPR > 8) v = dpp_add<DPP_ROW_MIRROR, 0xF>(v);
-                sum[r] = chunk == i ? v : sum[r];
-            }
-            if (col < p.cols) ((T *)p.out)[(t.row + r) * p.ldo + col] = (T)(none ? y[r] : y[r] + sum[r]);
-        }
+            for (int e = 0; e < EPL; e++) h[r][e] = (u32)r < t.rows ? hidden[r][lane % CPR * EPL + e] : 0.f;
+    }
+    for (; c0 < upto; c0 += step) {
+        if (!NEXT) few_load(p.u, t, c0, f[0]);
+        if (NEXT && c0 + step < upto) few_load(p.u, t, c0 + step, f[1 % (NEXT + 1)]);
+        few_store(p.u, t, c0, f[0], h);
+        if (NEXT) f[0] = f[1 % (NEXT + 1)];
     }
 }
 
@@ -1098,6 +1188,41 @@ Cut cut_of(const vms_lowrank_args *a, u64 in)
     return c;
 }
 
+// Requests of one token or two, of ranks that fill whole chunks, a power of two of them: the kernels without matrix units
+bool few_of(const vms_lowrank_args *a)
+{
+    const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
+    const u32 epl = 16 / type_bytes(a->dtype), chunks = a->rank / epl;
+    return each <= 2 && a->rank % epl == 0 && chunks <= 16 && (chunks & (chunks - 1)) == 0;
+}
+
+// tiles of FEW_ROWS rows that a batch can have
+u64 few_tiles(const vms_lowrank_args *a)
+{
+    const u64 tiles = a->d_starts ? a->rows / FEW_ROWS + a->n_requests + 2 : (a->rows + FEW_ROWS - 1) / FEW_ROWS;
+    return tiles < a->rows ? tiles : a->rows;
+}
+
+// Both products in one launch?  Where a workgroup has not too much of `in` to sum, again for each of a request's panels, and
+// every workgroup a place at once.  In 16 bits, 4096 -> 16384 at rank 16: 6.3 us for a token, 8.6 in two launches; 15.6 and 18.4
+// for 96 tokens, 38 and 64 for 500; 2048 -> 4096 at rank 64 8.0 and 8.0 for a token.  In 32 bits the matrix instructions of a
+// tile of one row take four times as long: 512 -> 2048 at rank 16 5.9 and 8.1 us, but 4096 -> 4096 12 and 9.6.
+bool one_launch(const vms_lowrank_args *a)
+{
+    return few_of(a) && few_tiles(a) <= OPS_CUS * 2 && padded_rank(a->rank) * a->in * type_bytes(a->dtype) <= (a->dtype == VMS_F32 ? 1u << 16 : 1u << 18);
+}
+
+// how the hidden values of the forward pass are made
+Cut forward_cut(const vms_lowrank_args *a)
+{
+    Cut c = cut_of(a, a->in);
+    if (one_launch(a)) {
+        c.splits = 1;
+        c.folded = false;
+    }
+    return c;
+}
+
 u32 planes_of(const vms_lowrank_args *a) { return a->dtype != VMS_F32 && a->rows * a->rank <= 1 << 16 ? 2 : 1; }
 
 // bytes of one layout with its planes
@@ -1139,14 +1264,9 @@ UpCut up_cut(const vms_lowrank_args *a, u64 cols, bool base)
 {
     UpCut c;
     const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
-    const u32 epl = 16 / type_bytes(a->dtype), chunks = a->rank / epl;
-    const bool few = each <= 2 && a->rank % epl == 0 && chunks <= 16 && (chunks & (chunks - 1)) == 0;
+    const bool few = few_of(a);
     c.tile16 = few ? 0 : each >= 512 && a->rank <= 64 && base ? 8 : each >= 48 ? 4 : 1;
-    u64 tiles = tiles_of(a, few ? 1 : c.tile16);
-    if (few) {
-        tiles = a->d_starts ? a->rows / FEW_ROWS + requests + 2 : (a->rows + FEW_ROWS - 1) / FEW_ROWS;
-        if (tiles > a->rows) tiles = a->rows;
-    }
+    const u64 tiles = few ? few_tiles(a) : tiles_of(a, c.tile16);
     c.tiles = (u32)tiles;
     const u64 trip = few ? 256 : (c.tile16 == 1 ? 4 : 1) * (SLAB_BYTES / type_bytes(a->dtype)), all = (cols + trip - 1) / trip;
     // Workgroups enough for four on every compute unit before one takes a second trip; no more than that where each has to
@@ -1220,6 +1340,28 @@ int down(const vms_lowrank_args *a, const Cut &c, const void *x, u64 ldx, const 
     rc = fold<T>(f, stream);
     h->parts = nullptr;
     return rc;
+}
+
+template <class T>
+int one(const vms_lowrank_args *a, const Hidden &h, void *stream)
+{
+    OneParams p = { { a->d_x, a->d_a, h, a->d_scales, requests_of(a), a->ldx, a->scale, (u32)a->in, a->rank },
+                    { h, a->d_b, a->d_y, a->d_out, requests_of(a), a->ldy, a->ldo, (u32)a->out, a->rank, 1, 1 } };
+    const u32 tiles = (u32)few_tiles(a), all = (u32)((a->out + ONE_WAVES * 64 - 1) / (ONE_WAVES * 64));
+    // Panels of columns: a workgroup for each compute unit, two where that leaves four trips for each (32 tokens, 4096 -> 16384
+    // at rank 16: 9.1 us with eight panels of four trips, 11.2 with 16 of two).
+    u32 panels = min(all / 4, OPS_CUS * 2 / tiles);
+    panels = max(max(panels, OPS_CUS / tiles), 1u);
+    p.u.trips = (all + panels - 1) / panels;
+    p.u.panels = (all + p.u.trips - 1) / p.u.trips;
+    const dim3 grid(tiles * p.u.panels), block(ONE_WAVES * 64);
+    switch (a->rank / Mma<T>::EPL) {
+    case 1: return ops_launch(lowrank_one_kernel<T, 1>, grid, block, 0, p, stream);
+    case 2: return ops_launch(lowrank_one_kernel<T, 2>, grid, block, 0, p, stream);
+    case 4: return ops_launch(lowrank_one_kernel<T, 4>, grid, block, 0, p, stream);
+    case 8: return ops_launch(lowrank_one_kernel<T, 8>, grid, block, 0, p, stream);
+    }
+    return ops_launch(lowrank_one_kernel<T, 16>, grid, block, 0, p, stream);
 }
 
 template <class T, int MR, int WR, bool ONCE = false>
@@ -1305,7 +1447,7 @@ Layout layout_of(const vms_lowrank_backward_args *a)
         *at = end;
         end += (bytes + 255) & ~(size_t)255;
     };
-    l.forward = cut_of(&f, f.in);
+    l.forward = forward_cut(&f);
     l.back = cut_of(&f, f.out);
     place(&l.at, a->d_dx ? (size_t)f.n_adapters * f.rank * f.in * e : 0);
     place(&l.bt, wants_hidden_gradient(a) ? (size_t)f.n_adapters * f.rank * f.out * e : 0);
@@ -1384,7 +1526,7 @@ __global__ __launch_bounds__(256) void lowrank_clear_kernel(const ClearParams p)
 extern "C" size_t vms_lowrank_hidden_bytes(const vms_lowrank_args *a)
 {
     if (check(a)) return 0;
-    return hidden_bytes(a, cut_of(a, a->in));
+    return hidden_bytes(a, forward_cut(a));
 }
 
 extern "C" int vms_lowrank(const vms_lowrank_args *a, void *stream)
@@ -1397,11 +1539,12 @@ extern "C" int vms_lowrank(const vms_lowrank_args *a, void *stream)
     if (!input_ok(a->d_y, a->dtype) || !near_ok(a->ldy) || !output_ok(a->d_out, a->dtype, a->ldo, a->out) || !near_ok(a->ldo)) return VMS_EINVAL;
     if (a->d_y == a->d_out && a->ldy != a->ldo) return VMS_EINVAL;
     if (!grid_ok(up_cut(a, a->out, true))) return VMS_EINVAL;
-    const Cut c = cut_of(a, a->in);
+    const Cut c = forward_cut(a);
     if (!grid_ok(c)) return VMS_EINVAL;
     Hidden h = hidden_at(a, c, a->d_hidden);
     return with_type(a->dtype, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
+        if (one_launch(a)) return one<T>(a, h, stream);
         const int r = down<T>(a, c, a->d_x, a->ldx, a->d_a, a->in, &h, stream);
         return r ? r : up<T>(a, h, a->d_b, a->d_y, a->ldy, a->d_out, a->ldo, a->out, stream);
     });

@@ -388,6 +388,25 @@ def test_long_sums_of_high_rank(dtype):
     check_low_rank(2100, 200, 4097, 100, dtype, 2, [0, 130, 2000], [1, 0], scale=[0.5, 2.0])
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rank", [4, 8, 16, 32, 64, 128])
+def test_single_tokens_in_one_launch_and_in_two(rank, dtype):
+    """One launch makes both products while `in` is short enough, by the padded rank; in panels of several trips if `out` is long"""
+    padded = max(rank, 16)
+    border = (1 << 16) // (4 * padded) if dtype == torch.float32 else (1 << 18) // (2 * padded)
+    starts = [1] + list(range(2, 41)) + [40, 42]
+    which = [i % 4 - 1 for i in range(len(starts) - 1)]
+    for k, n in ((border, 9000), (border + 1, 200), (min(border, 77), 4700)):
+        check_low_rank(43, k, n, rank, dtype, 3, starts, which, scale=[0.5, -1.0, 2.0], step=n == 200 or k == 77)
+        check_low_rank(2, k, n, rank, dtype, flat=True, step=n == 200)
+    check_low_rank(43, 77, 4700, rank, dtype, 3, starts, which, inplace=True, step=False)
+
+
+def test_single_tokens_of_more_requests_than_one_launch_takes():
+    for tokens in (500, 520):
+        check_low_rank(tokens, 72, 96, 16, torch.float16, 5, list(range(tokens + 1)), [i % 6 - 1 for i in range(tokens)])
+
+
 def test_single_tokens_through_wide_layers():
     for rank in (1, 16, 64):
         check_low_rank(1, 8192, 8192, rank, torch.bfloat16, step=False, flat=True)
