@@ -1149,14 +1149,16 @@ u64 tiles_of(const vms_lowrank_args *a, u32 tile16)
 const u32 DOWN_WAVES = 8;       // of a workgroup; twice that where the rank leaves the registers
 
 // Rows of a tile of `down`, in sixteens: no more than a request has on average, so that single tokens do not pay for rows that
-// are not there; at most four, two or one as the rank leaves registers; and fewer as long as there is not a tile for each
-// compute unit: larger tiles read the weights less often, but compute units without a tile read nothing.
+// are not there; at most four, two or one as the rank leaves registers; and half as many as long as there are then still no more
+// tiles than compute units: larger tiles read the weights less often, but compute units without a tile read nothing, and a few
+// tiles more than one for each take as long as two (24 requests of 6007 rows in all, 4096 -> 4096: rank 64 46 us forward with
+// tiles of 32 rows, 53 with 16; rank 32 41 and 44).
 u32 tile_of(const vms_lowrank_args *a)
 {
     const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
     u32 t = each >= 48 ? 4 : each >= 24 ? 2 : 1;
     t = a->rank > 64 ? 1 : a->rank > 32 && t > 2 ? 2 : t;
-    while (t > 1 && a->rows / (t * 16) < OPS_CUS) t /= 2;
+    while (t > 1 && tiles_of(a, t / 2) <= OPS_CUS) t /= 2;
     return t;
 }
 
