@@ -62,6 +62,36 @@ DI typename Some<T, N>::type load_first(const T *p, int n)
     return v;
 }
 
+// the same without a branch, for a row of N elements or more that ends n elements behind p: where those are fewer than N, the
+// row's last N, 0 in the place of those that p lies behind.  Which elements a sum takes in which place is all the same, as
+// long as both of its factors agree.
+template <int N, class T>
+DI typename Some<T, N>::type load_last(const T *p, int n)
+{
+    const int back = max(N - n, 0);
+    typename Some<T, N>::type v = load_some<N>(p - back);
+    const int PER = 4 / sizeof(T);          // elements of a register
+    u32 words[N / PER];
+    __builtin_memcpy(words, &v, sizeof v);
+#pragma unroll
+    for (int i = 0; i < N / PER; i++) words[i] &= back <= i * PER ? ~0u : back < (i + 1) * PER ? 0xFFFF0000u : 0u;
+    __builtin_memcpy(&v, words, sizeof v);
+    return v;
+}
+
+// the same for a shorter row
+template <int N, class T>
+DI typename Some<T, N>::type load_short(const T *p, int n)
+{
+    typename Some<T, N>::type v;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const T x = p[min(i, n - 1)];
+        v[i] = i < n ? x : (T)0.f;
+    }
+    return v;
+}
+
 // The lanes of a quad swap their registers: lane c's r[i] becomes lane i's r[c]
 template <class V>
 DI void quad_swap(V r[4])
@@ -227,8 +257,10 @@ struct DownParams {
     u32 in, rank;
 };
 
-// One slab of the summed dimension: 256 bytes of each row, of which `n` elements exist (WHOLE: all)
-template <class T, int MR, int NR, bool WHOLE>
+// One slab of the summed dimension: 256 bytes of each row, of which `n` elements exist (SLAB_WHOLE: all; SLAB_LAST: the end of
+// a row that is a load long or longer; SLAB_SHORT: a shorter row)
+enum Slab { SLAB_WHOLE, SLAB_LAST, SLAB_SHORT };
+template <class T, int MR, int NR, Slab KIND>
 DI void down_slab(const char *x, const char *w, const u32 (&xat)[MR][4], const u32 (&wat)[NR][4], int n, f32x4 (&acc)[MR][NR])
 {
     typedef typename Mma<T>::Frag Frag;
@@ -236,7 +268,10 @@ DI void down_slab(const char *x, const char *w, const u32 (&xat)[MR][4], const u
     const int SOME = NR < 4 ? NR : 4;       // of the rank's parts at a time; the registers do not hold more
     Frag a[MR][4], b[SOME][4];
     n -= (int)(slab_byte(lane_id()) / sizeof(T));
-    const auto load = [n](const char *p, u32 at) { return WHOLE ? load_some<EPL>((const T *)(p + at)) : load_first<EPL>((const T *)(p + at), n); };
+    const auto load = [n](const char *p, u32 at) {
+        const T *const from = (const T *)(p + at);
+        return KIND == SLAB_WHOLE ? load_some<EPL>(from) : KIND == SLAB_LAST ? load_last<EPL>(from, n) : load_short<EPL>(from, n);
+    };
 #pragma unroll
     for (int i = 0; i < MR; i++)
 #pragma unroll
@@ -268,8 +303,8 @@ DI void down_slab(const char *x, const char *w, const u32 (&xat)[MR][4], const u
     }
 }
 
-// A wavefront's share of the sums for a tile's MR x 16 rows and the whole rank: a slab in `shares`, and for the last one what
-// is left of a row.  Tiles begin at different places (`turn`): rows are often a power of two apart, so that what all tiles read
+// A wavefront's share of the sums for a tile's MR x 16 rows and the whole rank: a run of slabs (16384 x 4096 in 32 bits at rank
+// 16: 62 us, 69 with a slab in `shares`), and for the last one what is left of a row.  Tiles begin at different places (`turn`): rows are often a power of two apart, so that what all tiles read
 // at one place is in one channel of the caches.
 template <class T, int MR, int NR>
 DI void down_sums(const DownParams &p, const Tile &t, u32 share, u32 shares, u32 turn, f32x4 (&acc)[MR][NR])
@@ -291,12 +326,18 @@ DI void down_sums(const DownParams &p, const Tile &t, u32 share, u32 shares, u32
         for (int j = 0; j < NR; j++) acc[i][j] = f32x4{ 0.f, 0.f, 0.f, 0.f };
     const u32 slabs = p.in / SLAB;
     turn = slabs ? turn % slabs : 0;
-    for (u32 s = share; s < slabs; s += shares) {
+    const u32 run = (slabs + shares - 1) / shares, from = min(share * run, slabs), upto = min(from + run, slabs);
+    for (u32 s = from; s < upto; s++) {
         const u64 at = (u64)(s + turn < slabs ? s + turn : s + turn - slabs) * SLAB_BYTES;
-        down_slab<T, MR, NR, true>(x + at, w + at, xat, wat, 0, acc);
+        down_slab<T, MR, NR, SLAB_WHOLE>(x + at, w + at, xat, wat, 0, acc);
     }
-    if (share == shares - 1 && slabs * SLAB < p.in)
-        down_slab<T, MR, NR, false>(x + (u64)slabs * SLAB_BYTES, w + (u64)slabs * SLAB_BYTES, xat, wat, (int)(p.in - slabs * SLAB), acc);
+    if (share == shares - 1 && slabs * SLAB < p.in) {
+        const u64 at = (u64)slabs * SLAB_BYTES;
+        if (LIKELY(p.in >= (u32)Mma<T>::EPL))
+            down_slab<T, MR, NR, SLAB_LAST>(x + at, w + at, xat, wat, (int)(p.in - slabs * SLAB), acc);
+        else
+            down_slab<T, MR, NR, SLAB_SHORT>(x + at, w + at, xat, wat, (int)p.in, acc);
+    }
 }
 
 // MR x 16 rows and the whole rank in a workgroup; its WAVES wavefronts, and `splits` workgroups, share the summed dimension.
@@ -429,11 +470,11 @@ __global__ __launch_bounds__(512) void lowrank_down_shared_kernel(const DownPara
         const u64 at = (u64)slabs * SLAB_BYTES;
         const int n = mine ? 0 : (int)(p.in - slabs * SLAB), nx = n - (int)(slab_byte(lane) / sizeof(T));
 #pragma unroll
-        for (int i = 0; i < FILL; i++) fill[0][i] = load_first<EPL>((const T *)(w + at + wat[i]), n - (int)(local % 16 * EPL));
+        for (int i = 0; i < FILL; i++) fill[0][i] = load_last<EPL>((const T *)(w + at + wat[i]), n - (int)(local % 16 * EPL));
 #pragma unroll
         for (int i = 0; i < MR; i++)
 #pragma unroll
-            for (int u = 0; u < 4; u++) a[0][i][u] = load_first<EPL>((const T *)(x + at + xat[i][u]), nx);
+            for (int u = 0; u < 4; u++) a[0][i][u] = load_last<EPL>((const T *)(x + at + xat[i][u]), nx);
         Frag(&to)[CHUNKS] = panel[trips & 1][mine];
 #pragma unroll
         for (int i = 0; i < FILL; i++) to[place(i)] = fill[0][i];
