@@ -525,7 +525,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const NormJoinParams p)
 // any: 4099 rows of 5120 columns in 16 bits take 24 us with four wavefronts of three groups a lane, 28 with five of two; in 32
 // bits 42 with twelve of one, 45 with ten.
 // A workgroup for each row: many of them at different stages keep the memory busier than ones that stay and read a row ahead,
-// of which fewer fit (122 and 131 us for 16384 x 4096 in 16 bits with residual and dropout).
+// of which fewer fit (16384 x 4096 in 16 bits with residual and dropout take 113 us, 9 us more with such).
 template <class T, bool ONCE>
 int launch_norm(const NormParams &p, void *stream)
 {
