@@ -402,6 +402,22 @@ def test_single_tokens_in_one_launch_and_in_two(rank, dtype):
     check_low_rank(43, 77, 4700, rank, dtype, 3, starts, which, inplace=True, step=False)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("k", [2, 3, 4, 5, 7, 8, 9, 15, 65, 130, 1027])
+def test_ends_of_rows(k, dtype):
+    """Short rows, and rows whose end is read with elements that were counted before: an infinity there counts once"""
+    check_low_rank(37, k, 40, 12, dtype, flat=True)
+    check_low_rank(2, k, 40, 8, dtype, flat=True, step=False)
+    for rows in (1, 37):
+        wide = torch.full((rows, k + 16), float("nan"), dtype=dtype, device="cuda")
+        x = wide[:, 8:8 + k]
+        x.fill_(1.0)
+        x[:, max(k - 3, 0)] = float("inf")
+        a, b = torch.ones(8, k, dtype=dtype, device="cuda"), torch.ones(24, 8, dtype=dtype, device="cuda")
+        out = ops.low_rank_add(torch.zeros(rows, 24, dtype=dtype, device="cuda"), x, a, b)
+        assert (out == float("inf")).all()
+
+
 def test_single_tokens_of_more_requests_than_one_launch_takes():
     for tokens in (500, 520):
         check_low_rank(tokens, 72, 96, 16, torch.float16, 5, list(range(tokens + 1)), [i % 6 - 1 for i in range(tokens)])
