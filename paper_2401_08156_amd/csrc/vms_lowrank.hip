@@ -1044,9 +1044,9 @@ __global__ __launch_bounds__(256) void lowrank_outer_kernel(const OuterParams p)
     for (u32 base = 0; base < requests; base += 64) {
         u32 lo = 0, hi = 0;
         const u32 i = base + lane;
-        if (!p.q.starts) {
+        if (!p.q.starts) {          // one request, of adapter 0
             lo = from;
-            hi = lane ? from : upto;
+            hi = lane || adapter ? from : upto;
         } else if (i < requests && p.q.which[i] == (int)adapter) {
             request_rows(p.q, i, &lo, &hi);
             lo = max(lo, from);

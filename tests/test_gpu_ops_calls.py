@@ -1,0 +1,45 @@
+"""Calls of the operators that share memory, differentiate twice or leave gradients out, and the C entry points called with
+structures of one's own, against the oracle in 64 bits."""
+import ctypes
+
+import pytest
+import torch
+
+import ops_oracle as oo
+from paper_2401_08156_amd import ops
+from test_gpu_ops import TYPES, ids, normal
+
+pytestmark = pytest.mark.gpu
+CODES = {torch.float32: ops.VMS_F32, torch.float16: ops.VMS_F16, torch.bfloat16: ops.VMS_BF16}
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,rank", [(5, 16), (300, 8), (2100, 64)])
+def test_without_starts_all_rows_are_adapter_0s(rows, rank, dtype):
+    """The C entry points take several adapters without starts: those beyond the first have no rows, and gradients of 0"""
+    k, n, adapters = 136, 200, 3
+    (x, x64), (y, y64), (dout, dout64) = [normal((rows, c), dtype, s) for c, s in ((k, 1), (n, 2), (n, 5))]
+    a, a64 = normal((adapters, rank, k), dtype, 3, k ** -0.5)
+    b, b64 = normal((adapters, n, rank), dtype, 4, rank ** -0.5)
+    want = oo.low_rank(dtype, y64, x64, a64, b64, [0.5] * adapters, [0, rows], [0], dout64)
+    f = ops.vms_lowrank_args(152, CODES[dtype], rows, k, n, rank, adapters, 0, 0.5, None, x.data_ptr(), y.data_ptr(), a.data_ptr(), b.data_ptr(),
+                             None, None, None, k, n, n, None, 0)
+    L = ops.lib()
+    f.hidden_bytes = L.vms_lowrank_hidden_bytes(ctypes.byref(f))
+    hidden = torch.empty(f.hidden_bytes, dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(y)
+    f.d_hidden, f.d_out = hidden.data_ptr(), out.data_ptr()
+    assert L.vms_lowrank(ctypes.byref(f), stream()) == 0
+    dx, da, db = [torch.full_like(t, float("nan")) for t in (x, a, b)]
+    g = ops.vms_lowrank_backward_args(224, 0, f, dout.data_ptr(), dx.data_ptr(), da.data_ptr(), db.data_ptr(), n, k, None, 0)
+    g.workspace_bytes = L.vms_lowrank_backward_workspace_bytes(ctypes.byref(g))
+    workspace = torch.empty(g.workspace_bytes, dtype=torch.uint8, device="cuda")
+    g.d_workspace = workspace.data_ptr()
+    assert L.vms_lowrank_backward(ctypes.byref(g), stream()) == 0
+    for name, got in (("out", out), ("dx", dx), ("da", da), ("db", db)):
+        oo.assert_within(name, got, *want[name])
+    assert not da[1:].any() and not db[1:].any()
