@@ -366,6 +366,24 @@ std::pair<Tensor, Tensor> run_low_rank(const Tensor &y, const Tensor &x, const T
     return { out, hidden };
 }
 
+// May an element of t lie in the memory of y, a matrix of rows of its own?  Columns of one matrix beside each other may not.
+bool shares(const Tensor &y, const Tensor &t)
+{
+    if (!t.defined() || !y.numel() || !t.numel()) return false;
+    const auto begin = [](const Tensor &v) { return (uintptr_t)v.const_data_ptr(); };
+    const auto size = [](const Tensor &v) {         // bytes from the first element to behind the last
+        int64_t last = 0;
+        for (int64_t i = 0; i < v.dim(); i++) last += (v.size(i) - 1) * v.stride(i);
+        return (uintptr_t)(last + 1) * v.element_size();
+    };
+    if (begin(t) >= begin(y) + size(y) || begin(y) >= begin(t) + size(t)) return false;
+    const Matrix m = matrix(y), k = matrix(t);
+    if (!k.t.is_same(t) || k.ld != m.ld || t.element_size() != y.element_size()) return true;
+    const uint64_t row = m.ld * y.element_size();
+    const uint64_t at = begin(t) >= begin(y) ? (begin(t) - begin(y)) % row : (row - (begin(y) - begin(t)) % row) % row;     // in a row of y
+    return at < columns(y) * y.element_size() || at + columns(t) * t.element_size() > row;
+}
+
 struct LowRankAdd : torch::autograd::Function<LowRankAdd> {
     static Tensor forward(AutogradContext *ctx, const Tensor &y, const Tensor &x, const Tensor &a, const Tensor &b, const Batch &batch, bool inplace)
     {
@@ -408,21 +426,21 @@ struct LowRankAdd : torch::autograd::Function<LowRankAdd> {
     }
 };
 
-Tensor low_rank_add(const Tensor &y, const Tensor &x, const Tensor &a_, const Tensor &b_, const py::object &scale, const std::optional<Tensor> &starts_,
+Tensor low_rank_add(const Tensor &y, const Tensor &x_, const Tensor &a_, const Tensor &b_, const py::object &scale, const std::optional<Tensor> &starts_,
                     const std::optional<Tensor> &which_, bool inplace)
 {
     const Tensor starts = starts_.value_or(Tensor()), which = which_.value_or(Tensor());
-    same(x, { &y, &a_, &b_ });
-    if (!x.dim() || x.dim() != y.dim() || x.sizes().slice(0, x.dim() - 1) != y.sizes().slice(0, y.dim() - 1)) refuse("x and y have different rows");
+    same(x_, { &y, &a_, &b_ });
+    if (!x_.dim() || x_.dim() != y.dim() || x_.sizes().slice(0, x_.dim() - 1) != y.sizes().slice(0, y.dim() - 1)) refuse("x and y have different rows");
     if (a_.dim() != b_.dim() || (a_.dim() != 2 && a_.dim() != 3)) refuse("a is [rank, in] and b [out, rank], or both with the adapters in front");
     const int64_t rank = a_.size(-2), adapters = a_.dim() == 3 ? a_.size(0) : 1;
-    if ((a_.dim() == 3 && b_.size(0) != adapters) || rank != b_.size(-1) || a_.size(-1) != x.size(-1) || b_.size(-2) != y.size(-1))
-        refuse("a and b do not lead from " + std::to_string(x.size(-1)) + " to " + std::to_string(y.size(-1)) + " features by the same rank and adapters");
+    if ((a_.dim() == 3 && b_.size(0) != adapters) || rank != b_.size(-1) || a_.size(-1) != x_.size(-1) || b_.size(-2) != y.size(-1))
+        refuse("a and b do not lead from " + std::to_string(x_.size(-1)) + " to " + std::to_string(y.size(-1)) + " features by the same rank and adapters");
     if (rank < 1 || rank > VMS_LOWRANK_MAX_RANK) refuse("ranks from 1 to " + std::to_string(VMS_LOWRANK_MAX_RANK) + ", got " + std::to_string(rank));
     if (starts.defined() != which.defined()) refuse("starts and which come together");
     if (!starts.defined() && adapters != 1) refuse("several adapters need starts and which");
     for (const Tensor *t : { &starts, &which })
-        if (t->defined() && (t->scalar_type() != at::kInt || t->device() != x.device() || t->dim() != 1 || !t->is_contiguous()))
+        if (t->defined() && (t->scalar_type() != at::kInt || t->device() != x_.device() || t->dim() != 1 || !t->is_contiguous()))
             refuse("starts and which are contiguous int32 vectors on the input's device");
     if (starts.defined() && starts.numel() != which.numel() + 1)
         refuse(std::to_string(which.numel()) + " requests have one start more, not " + std::to_string(starts.numel()));
@@ -430,7 +448,7 @@ Tensor low_rank_add(const Tensor &y, const Tensor &x, const Tensor &a_, const Te
     Tensor scales;
     if (THPVariable_Check(scale.ptr())) {
         scales = py::cast<Tensor>(scale);
-        if (scales.scalar_type() != at::kFloat || scales.device() != x.device() || scales.dim() != 1 || scales.size(0) != adapters || !scales.is_contiguous())
+        if (scales.scalar_type() != at::kFloat || scales.device() != x_.device() || scales.dim() != 1 || scales.size(0) != adapters || !scales.is_contiguous())
             refuse("a scale tensor is a contiguous float32 vector with one number for each adapter");
         if (scales.requires_grad()) refuse("scales have no gradient");
     } else {
@@ -443,8 +461,10 @@ Tensor low_rank_add(const Tensor &y, const Tensor &x, const Tensor &a_, const Te
     if (inplace && !matrix(y, LOWRANK_FAR).t.is_same(y)) refuse("y's strides do not allow the sum in place");
     if (inplace && at::GradMode::is_enabled() && y.requires_grad() && y.is_leaf()) refuse("the sum in place of a leaf that requires a gradient");
     const py::gil_scoped_release go;
-    const Tensor a = a_.contiguous(), b = b_.contiguous();
-    const Batch batch = { factor, scales, starts, which };
+    // What lies in the memory that the sum goes to is read from a copy: workgroups write columns of a row whose x others still read
+    const auto apart = [&](const Tensor &t) { return inplace && shares(y, t) ? t.clone() : t; };
+    const Tensor x = apart(x_), a = apart(a_).contiguous(), b = apart(b_).contiguous();
+    const Batch batch = { factor, apart(scales), apart(starts), apart(which) };
     if (wanted({ &y, &x, &a, &b })) return LowRankAdd::apply(y, x, a, b, batch, inplace);
     const Tensor out = run_low_rank(y, x, a, b, batch, inplace).first;
     if (inplace) y.unsafeGetTensorImpl()->bump_version();       // as a node's mark_dirty does: what was saved of y is noticed

@@ -136,6 +136,7 @@ def low_rank_add(y, x, a, b, scale=1.0, starts=None, which=None, inplace=False):
     before starts[0] and from starts[-1] on belong to no request, and their sum is y.  `scale` is a number or a float32
     tensor with one for each adapter.  Ranks up to 128, requests up to 65535.
 
-    `inplace` makes the sum in y itself and leaves rows of no request untouched.  Gradients: of y, x, a and b; an
+    `inplace` makes the sum in y itself and leaves rows of no request untouched; what lies in y's memory of the other tensors
+    (x may be y) is copied first.  Gradients: of y, x, a and b; an
     adapter's are summed over all its requests.  Kept for the backward pass: x, a, b, and scale * x a^T."""
     return (_nodes or nodes()).low_rank_add(y, x, a, b, scale, starts, which, inplace)

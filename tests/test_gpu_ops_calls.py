@@ -43,3 +43,51 @@ def test_without_starts_all_rows_are_adapter_0s(rows, rank, dtype):
     for name, got in (("out", out), ("dx", dx), ("da", da), ("db", db)):
         oo.assert_within(name, got, *want[name])
     assert not da[1:].any() and not db[1:].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows", [1, 3, 700])
+def test_the_sum_in_place_of_its_own_input(rows, dtype):
+    """x is y, a part of y or the adapters are: what is read is what lay there before the sum"""
+    n, rank = 640, 16
+    (v, v64), (a, a64), (b, b64) = normal((rows, n), dtype, 1), normal((rank, n), dtype, 2, n ** -0.5), normal((n, rank), dtype, 3, rank ** -0.5)
+    want = oo.low_rank(dtype, v64, v64, a64[None], b64[None], [0.5])["out"]
+    y = v.clone()
+    assert ops.low_rank_add(y, y, a, b, 0.5, inplace=True) is y
+    oo.assert_within("x is y", y, *want)
+    y = v.clone()
+    ops.low_rank_add(y, y.view(rows, n), a, b, 0.5, inplace=True)
+    oo.assert_within("a view", y, *want)
+    # rows of y shifted by one: row i + 1 is y's and row i + 1 of x
+    wide, wide64 = normal((rows + 1, n), dtype, 4)
+    want = oo.low_rank(dtype, wide64[1:], wide64[:-1], a64[None], b64[None], [0.5])["out"]
+    ops.low_rank_add(wide[1:], wide[:-1], a, b, 0.5, inplace=True)
+    oo.assert_within("shifted rows", wide[1:], *want)
+    # a inside y
+    y, y64 = normal((rank, n), dtype, 5)
+    x, x64 = normal((rank, n), dtype, 6)
+    want = oo.low_rank(dtype, y64, x64, y64[None], b64[None], [0.5])["out"]
+    ops.low_rank_add(y, x, y, b, 0.5, inplace=True)
+    oo.assert_within("a is y", y, *want)
+    # beside each other in one matrix, and apart
+    wide, wide64 = normal((rows, 2 * n), dtype, 7)
+    want = oo.low_rank(dtype, wide64[:, :n], wide64[:, n:], a64[None], b64[None], [0.5])["out"]
+    ops.low_rank_add(wide[:, :n], wide[:, n:], a, b, 0.5, inplace=True)
+    oo.assert_within("columns beside", wide[:, :n], *want)
+    assert torch.equal(wide[:, n:].cpu().double(), wide64[:, n:])
+
+
+@pytest.mark.parametrize("rows", [2, 300])
+def test_gradients_of_the_sum_in_place_of_its_own_input(rows):
+    dtype, n, rank = torch.float32, 96, 8
+    (v, v64), (a, a64), (b, b64), (dout, dout64) = normal((rows, n), dtype, 1), normal((rank, n), dtype, 2, n ** -0.5), normal((n, rank), dtype, 3, rank ** -0.5), normal((rows, n), dtype, 4)
+    for t in (v, a, b):
+        t.requires_grad_(True)
+    y = v * 1.0
+    out = ops.low_rank_add(y, y, a, b, 0.5, inplace=True)
+    got = torch.autograd.grad(out, (v, a, b), dout)
+    want = oo.low_rank(dtype, v64, v64, a64[None], b64[None], [0.5], dout=dout64)
+    oo.assert_within("out", out, *want["out"])
+    oo.assert_within("dx", got[0], want["dx"][0] + dout64, want["dx"][1] + oo.E32 * (want["dx"][0] + dout64).abs())
+    oo.assert_within("da", got[1], want["da"][0][0], want["da"][1][0])
+    oo.assert_within("db", got[2], want["db"][0][0], want["db"][1][0])
