@@ -4,7 +4,10 @@
 // calls: a node in Python took 23 us of the host's time forward and 27 us backward on a thread that autograd wakes for
 // it, the kernels 8 us.
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/impl/LocalDispatchKeySet.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/extension.h>
 
 #include "../../include/vms_ops.h"
@@ -48,9 +51,22 @@ uint32_t type_of(const Tensor &x)
     }
 }
 
+// The kernels are called past PyTorch's dispatcher: a trace would hold an output that nothing fills, and a tangent would end here.
+void refuse_followers(std::initializer_list<const Tensor *> tensors)
+{
+    using c10::impl::TorchDispatchModeTLS;
+    if (torch::jit::tracer::isTracing() || TorchDispatchModeTLS::get_mode(c10::impl::TorchDispatchModeKey::PROXY) ||
+        c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::PreDispatch))
+        refuse("these operators cannot be traced");
+    for (const Tensor *t : tensors)
+        if (t->defined() && t->_fw_grad(0).defined()) refuse("these operators have no forward-mode gradients");
+}
+
 // every other tensor has x's type and device
 void same(const Tensor &x, std::initializer_list<const Tensor *> others)
 {
+    refuse_followers({ &x });
+    refuse_followers(others);
     type_of(x);
     if (!x.is_cuda()) refuse("tensors on a GPU, got one on " + x.device().str());
     for (const Tensor *t : others)
@@ -450,6 +466,7 @@ Tensor low_rank_add(const Tensor &y, const Tensor &x_, const Tensor &a_, const T
         scales = py::cast<Tensor>(scale);
         if (scales.scalar_type() != at::kFloat || scales.device() != x_.device() || scales.dim() != 1 || scales.size(0) != adapters || !scales.is_contiguous())
             refuse("a scale tensor is a contiguous float32 vector with one number for each adapter");
+        refuse_followers({ &scales });
         if (scales.requires_grad()) refuse("scales have no gradient");
     } else {
         factor = PyFloat_AsDouble(scale.ptr());

@@ -10,7 +10,8 @@ tensors.  What is kept for the backward pass is named with each operator; a forw
 recomputation does, gives the same bits.  Gradients are summed in a fixed order.
 
 The kernels of libvmsreplay.so do all the work, called from the autograd nodes of _vms_torch.so (csrc/vms_torch_ops.cpp):
-wrong arguments raise ValueError or VmsError, and there is no other path for tensors that are not on a GPU.  The structures
+wrong arguments raise ValueError or VmsError, and there is no other path for tensors that are not on a GPU.  PyTorch does not
+see what they compute: traces (torch.jit.trace, make_fx) and forward-mode gradients are refused.  The structures
 below are those of the C entry points, for programs that call them with pointers of their own.
 
 Tensors may have any strides.  Rows (the last dimension) that are not consecutive in memory, leading dimensions that are not
