@@ -7,6 +7,7 @@
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/extension.h>
 
@@ -120,19 +121,30 @@ bool wanted(std::initializer_list<const Tensor *> tensors)
     return false;
 }
 
-// Gradients of gradients: where they are asked for (create_graph), what a backward pass returns is a node that refuses
-struct FirstOrder : torch::autograd::Function<FirstOrder> {
-    static Tensor forward(AutogradContext *, const Tensor &gradient, const Tensor &) { return gradient.detach(); }
-    static variable_list backward(AutogradContext *, variable_list) { TORCH_CHECK(false, "these operators have gradients of first order only"); }
+// Gradients of gradients: where they are asked for (create_graph), what a backward pass returns goes on from a node that refuses,
+// as a function of the gradients that arrived and of those inputs of the operator that it varies with (`by`: a bit for each
+// input, for each gradient).
+struct FirstOrder : torch::autograd::Node {
+    variable_list apply(variable_list &&) override { TORCH_CHECK(false, "these operators have gradients of first order only"); }
 };
 
-variable_list first_order(variable_list grads, const variable_list &from)
+variable_list first_order(variable_list grads, const variable_list &from, std::initializer_list<uint32_t> by)
 {
-    if (at::GradMode::is_enabled())
-        for (Tensor &g : grads)
-            if (g.defined())
-                for (const Tensor &f : from)
-                    if (f.defined() && f.requires_grad()) g = FirstOrder::apply(g.is_same(f) ? g.detach() : g, f);
+    if (!at::GradMode::is_enabled()) return grads;
+    const auto here = torch::autograd::get_current_node();
+    for (size_t i = 0; i < by.size(); i++) {
+        if (!grads[i].defined()) continue;
+        torch::autograd::edge_list edges;
+        for (const Tensor &f : from)
+            if (f.defined() && f.requires_grad()) edges.push_back(torch::autograd::impl::gradient_edge(f));
+        for (uint32_t k = 0; k < here->num_outputs(); k++)
+            if ((by.begin()[i] >> k & 1) && here->next_edge(k).is_valid()) edges.push_back(here->next_edge(k));
+        if (edges.empty()) continue;
+        const auto node = std::make_shared<FirstOrder>();
+        node->set_next_edges(std::move(edges));
+        grads[i] = grads[i].detach();
+        torch::autograd::set_history(grads[i], node);
+    }
     return grads;
 }
 
@@ -208,7 +220,7 @@ struct Dropout : torch::autograd::Function<Dropout> {
             dx = run_dropout(dy, {}, mask);
         }
         const bool residual = ctx->saved_data["residual"].toBool() && ctx->needs_input_grad(1);
-        return first_order({ dx, residual ? dy : Tensor(), {}, {}, {} }, grads);
+        return first_order({ dx, residual ? dy : Tensor(), {}, {}, {} }, grads, { 0, 0 });
     }
 };
 
@@ -304,7 +316,8 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
         none[1] = dweight;
         none[2] = dbias;
         if (need_r) none[3] = dres;
-        return first_order(none, grads);
+        const uint32_t sum = 1 | (there & 4 ? 1u << (input - 1) : 0), all = sum | (there & 1 ? 2 : 0);     // inputs that make up s, and with the weight
+        return first_order(none, grads, { all, sum, 0, all });
     }
 };
 
@@ -438,7 +451,7 @@ struct LowRankAdd : torch::autograd::Function<LowRankAdd> {
             g.d_workspace = workspace.data_ptr();
             call(vms_lowrank_backward, "vms_lowrank_backward", g, x);
         }
-        return first_order({ need_y ? dout : Tensor(), dx, da, db, {}, {} }, grads);
+        return first_order({ need_y ? dout : Tensor(), dx, da, db, {}, {} }, grads, { 0, 0xC, 0xA, 0x6 });
     }
 };
 

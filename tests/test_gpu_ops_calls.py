@@ -91,3 +91,28 @@ def test_gradients_of_the_sum_in_place_of_its_own_input(rows):
     oo.assert_within("dx", got[0], want["dx"][0] + dout64, want["dx"][1] + oo.E32 * (want["dx"][0] + dout64).abs())
     oo.assert_within("da", got[1], want["da"][0][0], want["da"][1][0])
     oo.assert_within("db", got[2], want["db"][0][0], want["db"][1][0])
+
+
+def test_gradients_of_gradients_are_refused_where_the_upper_one_is_constant():
+    """dout needs no gradient, but dx goes by the weights, and theirs by x"""
+    new = lambda *s: torch.randn(s, device="cuda", requires_grad=True)
+    x, r, w, b = new(8, 16), new(8, 16), new(16), new(16)
+    la, lb, base = new(4, 16), new(16, 4), new(8, 16)
+    one = torch.ones(8, 16, device="cuda")
+
+    def outputs():
+        yield "norm", lambda: ops.layer_norm(x, w, b), (x, w)
+        yield "norm of a sum", lambda: sum(ops.layer_norm(x, w, b, residual=r, p=0.2, seed=1)), (x, r, w)
+        yield "adapters", lambda: ops.low_rank_add(base, x, la, lb), (x, la, lb)
+    for name, make, leaves in outputs():
+        for leaf in leaves:
+            g, = torch.autograd.grad(make(), leaf, one, create_graph=True)
+            with pytest.raises(RuntimeError, match="first order"):
+                ((g * g).sum() + sum(v.sum() for v in leaves)).backward()
+    # what does not depend on them has a gradient that is a constant
+    for y, leaf in ((ops.dropout(x, 0.5, 1), x), (ops.layer_norm(x, w, b), b), (ops.low_rank_add(base, x, la, lb), base)):
+        g, = torch.autograd.grad(y, leaf, one, create_graph=True)
+        assert not g.requires_grad
+    frozen = ops.low_rank_add(base, x.detach(), la, lb.detach())
+    g, = torch.autograd.grad(frozen, la, one, create_graph=True)
+    assert not g.requires_grad
