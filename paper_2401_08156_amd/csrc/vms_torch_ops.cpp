@@ -278,7 +278,7 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
         variable_list none(8);
-        Tensor dy = grads[0];
+        const Tensor &dy = grads[0];
         const Tensor ds = grads.size() > 1 ? grads[1] : Tensor();
         if (!dy.defined() && !ds.defined()) return none;
         const auto saved = ctx->get_saved_variables();
@@ -289,21 +289,31 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
         size_t input = 1;               // inputs are numbered without those that are not there
         const auto need = [&](int64_t bit) { return (there & bit) && ctx->needs_input_grad(input++); };
         const bool need_x = ctx->needs_input_grad(0), need_w = need(1), need_b = need(2), need_r = need(4);
+        const auto options = s.options().requires_grad(false);
+        const Seed seed = { (uint64_t)ctx->saved_data["seed"].toInt(), saved[3] };
+        const vms_dropout_mask mask = mask_of(p, seed, (uint64_t)ctx->saved_data["call"].toInt());
+        if (!dy.defined()) {            // only s is used: rows without a norm have this gradient all the same
+            if (need_x) {
+                const at::NoGradGuard guard;
+                none[0] = p > 0.0 ? run_dropout(ds, {}, mask) : ds;
+            }
+            if (need_w) none[1] = at::zeros({ (int64_t)columns(s) }, options);
+            if (need_b) none[2] = at::zeros({ (int64_t)columns(s) }, options);
+            if (need_r) none[3] = ds;
+            return first_order(none, grads, { 0, 0, 0, 0 });
+        }
         {
             const at::NoGradGuard guard;
-            if (!dy.defined()) dy = at::zeros_like(s);
             const uint64_t n = rows(s), cols = columns(s);
-            const auto options = s.options().requires_grad(false);
             dres = like(s);
             if (p > 0.0 && need_x) dx = like(s);
             if (need_w) dweight = at::empty({ (int64_t)cols }, options);
             if (need_b) dbias = at::empty({ (int64_t)cols }, options);
             const Matrix m = matrix(dy), e = matrix(ds), k = matrix(s);
             const Tensor w = weight.defined() ? weight.contiguous() : weight;
-            const Seed seed = { (uint64_t)ctx->saved_data["seed"].toInt(), saved[3] };
             vms_layernorm_backward_args a = { sizeof a, type_of(s), n, cols, m.ptr(), e.ptr(), k.ptr(), ptr(w), (const float *)ptr(saved[1]), dres.data_ptr(),
                                               ptr(dx), ptr(dweight), ptr(dbias), m.ld, e.ld, k.ld, cols, cols,
-                                              mask_of(p, seed, (uint64_t)ctx->saved_data["call"].toInt()), nullptr, 0 };
+                                              mask, nullptr, 0 };
             Tensor workspace;
             a.workspace_bytes = vms_layernorm_backward_workspace_bytes(&a);
             if (a.workspace_bytes) {

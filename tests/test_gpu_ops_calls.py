@@ -116,3 +116,28 @@ def test_gradients_of_gradients_are_refused_where_the_upper_one_is_constant():
     frozen = ops.low_rank_add(base, x.detach(), la, lb.detach())
     g, = torch.autograd.grad(frozen, la, one, create_graph=True)
     assert not g.requires_grad
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+def test_where_only_the_sum_is_used_the_norm_has_no_part_in_the_gradient(dtype):
+    """Rows of infinities, NaN, or of equal values with eps = 0 have no norm; the sum's gradient does not go by it"""
+    x, r, ds = [normal((9, 200), dtype, s)[0] for s in (1, 2, 3)]
+    r[1, 5], r[2, 7] = float("inf"), float("nan")
+    x[3], r[3] = 0.0, 2.0
+    w, b = [torch.ones(200, dtype=dtype, device="cuda", requires_grad=True) for _ in range(2)]
+    x.requires_grad_(True)
+    r.requires_grad_(True)
+    y, s = ops.layer_norm(x, w, b, 0.0, residual=r, p=0.3, seed=4, call=5)
+    dx, dr, dw, db = torch.autograd.grad(s, (x, r, w, b), ds)
+    assert torch.equal(dr, ds) and torch.equal(dx, ops.dropout(ds, 0.3, 4, 5)) and not dw.any() and not db.any()
+    y, s = ops.layer_norm(x, residual=r)
+    dx, dr = torch.autograd.grad(s, (x, r), ds)
+    assert torch.equal(dr, ds) and torch.equal(dx, ds)
+    # its gradient goes by the one that arrived, which is refused as everywhere
+    s = ops.layer_norm(x, residual=r, p=0.3, seed=4)[1]
+    for leaf in (x, r):
+        g, = torch.autograd.grad((s * s).sum(), leaf, create_graph=True)
+        with pytest.raises(RuntimeError, match="first order"):
+            torch.autograd.grad(g.sum(), leaf)
+    s = ops.layer_norm(x, residual=r, p=0.3, seed=4)[1]
+    assert not torch.autograd.grad(s, x, ds, create_graph=True)[0].requires_grad
