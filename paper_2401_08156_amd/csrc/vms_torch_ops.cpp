@@ -79,6 +79,7 @@ void same(const Tensor &x, std::initializer_list<const Tensor *> others)
 // a tensor as rows of its last dimension; a copy where its strides do not allow that, or rows are `far` elements apart
 // (what the library's entry points refuse)
 const uint64_t FAR = 1ull << 31, LOWRANK_FAR = 1ull << 23;
+const int64_t MOST = 65535;         // adapters and requests of a call
 struct Matrix {
     Tensor t;
     uint64_t ld = 0;
@@ -476,6 +477,8 @@ Tensor low_rank_add(const Tensor &y, const Tensor &x_, const Tensor &a_, const T
     if ((a_.dim() == 3 && b_.size(0) != adapters) || rank != b_.size(-1) || a_.size(-1) != x_.size(-1) || b_.size(-2) != y.size(-1))
         refuse("a and b do not lead from " + std::to_string(x_.size(-1)) + " to " + std::to_string(y.size(-1)) + " features by the same rank and adapters");
     if (rank < 1 || rank > VMS_LOWRANK_MAX_RANK) refuse("ranks from 1 to " + std::to_string(VMS_LOWRANK_MAX_RANK) + ", got " + std::to_string(rank));
+    if (adapters > MOST || (which.defined() && which.numel() > MOST))       // (before they are counted in 32 bits)
+        refuse("up to " + std::to_string(MOST) + " adapters and requests, got " + std::to_string(adapters) + " and " + std::to_string(which.defined() ? which.numel() : 1));
     if (starts.defined() != which.defined()) refuse("starts and which come together");
     if (!starts.defined() && adapters != 1) refuse("several adapters need starts and which");
     for (const Tensor *t : { &starts, &which })

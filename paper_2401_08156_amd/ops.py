@@ -135,7 +135,7 @@ def low_rank_add(y, x, a, b, scale=1.0, starts=None, which=None, inplace=False):
     out, rank], and the rows of x and y packed by request: request i has rows starts[i] to starts[i + 1] - 1 and adapter
     which[i] (none if that is negative), with `starts` and `which` int32 on the device.  `starts` does not decrease; rows
     before starts[0] and from starts[-1] on belong to no request, and their sum is y.  `scale` is a number or a float32
-    tensor with one for each adapter.  Ranks up to 128, requests up to 65535.
+    tensor with one for each adapter.  Ranks up to 128, adapters and requests up to 65535.
 
     `inplace` makes the sum in y itself and leaves rows of no request untouched; what lies in y's memory of the other tensors
     (x may be y) is copied first.  Gradients: of y, x, a and b; an

@@ -141,3 +141,15 @@ def test_where_only_the_sum_is_used_the_norm_has_no_part_in_the_gradient(dtype):
             torch.autograd.grad(g.sum(), leaf)
     s = ops.layer_norm(x, residual=r, p=0.3, seed=4)[1]
     assert not torch.autograd.grad(s, x, ds, create_graph=True)[0].requires_grad
+
+
+def test_numbers_of_adapters_and_requests_beyond_32_bits_are_refused():
+    x, y = torch.zeros(4, 8, device="cuda"), torch.zeros(4, 8, device="cuda")
+    i = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    a, b = torch.zeros(1, 1, 8, device="cuda"), torch.zeros(1, 8, 1, device="cuda")
+    for n in (65536, (1 << 32) + 1):
+        with pytest.raises((ValueError, ops.VmsError)):
+            ops.low_rank_add(y, x, a.expand(n, 1, 8), b.expand(n, 8, 1), starts=i(0, 4), which=i(0))
+    many = torch.empty((1 << 32) + 2, dtype=torch.int32, device="cuda")        # (refused before a number is read)
+    with pytest.raises((ValueError, ops.VmsError)):
+        ops.low_rank_add(y, x, a, b, starts=many, which=many[:-1])
