@@ -7,6 +7,7 @@
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/VariableTypeUtils.h>
 #include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/extension.h>
@@ -503,6 +504,13 @@ Tensor low_rank_add(const Tensor &y, const Tensor &x_, const Tensor &a_, const T
     }
     if (inplace && !matrix(y, LOWRANK_FAR).t.is_same(y)) refuse("y's strides do not allow the sum in place");
     if (inplace && at::GradMode::is_enabled() && y.requires_grad() && y.is_leaf()) refuse("the sum in place of a leaf that requires a gradient");
+    if (inplace) {          // what autograd would refuse when the sum is made already
+        const bool node = wanted({ &y, &x_, &a_, &b_ });
+        if (y.is_inference() && !c10::InferenceMode::is_enabled()) refuse("the sum in place of an inference tensor outside inference mode");
+        for (const Tensor *t : std::initializer_list<const Tensor *>{ &x_, &a_, &b_, &scales, &starts, &which })
+            if (node && t->defined() && t->is_inference()) refuse("inference tensors are not kept for a backward pass");
+        torch::autograd::check_inplace(y, node);
+    }
     const py::gil_scoped_release go;
     // What lies in the memory that the sum goes to is read from a copy: workgroups write columns of a row whose x others still read
     const auto apart = [&](const Tensor &t) { return inplace && shares(y, t) ? t.clone() : t; };

@@ -153,3 +153,27 @@ def test_numbers_of_adapters_and_requests_beyond_32_bits_are_refused():
     many = torch.empty((1 << 32) + 2, dtype=torch.int32, device="cuda")        # (refused before a number is read)
     with pytest.raises((ValueError, ops.VmsError)):
         ops.low_rank_add(y, x, a, b, starts=many, which=many[:-1])
+
+
+def test_a_sum_in_place_that_autograd_forbids_changes_nothing():
+    x, a, b = torch.randn(5, 64, device="cuda"), torch.randn(8, 64, device="cuda", requires_grad=True), torch.randn(64, 8, device="cuda")
+    leaf = torch.randn(9, 64, device="cuda", requires_grad=True)
+    parts = (torch.randn(10, 64, device="cuda") * leaf[:1]).split(5)       # views that share their history
+    with torch.inference_mode():
+        inner = torch.randn(5, 64, device="cuda")
+    for y in (leaf[:5], parts[0], inner):
+        before = y.detach().clone()
+        with pytest.raises((RuntimeError, ValueError)):
+            ops.low_rank_add(y, x, a, b, inplace=True)
+        assert torch.equal(y.detach(), before)
+    before = inner.clone()
+    with torch.no_grad(), pytest.raises((RuntimeError, ValueError), match="inference"):
+        ops.low_rank_add(inner, x, a, b, inplace=True)
+    assert torch.equal(inner, before)
+    y = x.clone()
+    with pytest.raises((RuntimeError, ValueError), match="[Ii]nference"):
+        ops.low_rank_add(y, inner, a, b, inplace=True)
+    assert torch.equal(y, x)
+    with torch.inference_mode():
+        want = ops.low_rank_add(inner, x, a, b)
+        assert ops.low_rank_add(inner, x, a, b, inplace=True) is inner and torch.equal(inner, want)
