@@ -87,9 +87,13 @@ struct Matrix {
     const void *ptr() const { return t.defined() ? t.const_data_ptr() : nullptr; }
 };
 
+// (what lies in the memory of a negative view, as of a conjugate's imaginary part, is not its values)
+Tensor flat(const Tensor &t) { return t.defined() ? t.resolve_neg().contiguous() : t; }
+
 Matrix matrix(const Tensor &t, uint64_t far = FAR)
 {
     if (!t.defined()) return {};
+    if (t.is_neg()) return matrix(flat(t), far);
     const int64_t n = t.dim(), cols = t.size(-1);
     if (t.is_contiguous()) return { t, (uint64_t)cols };
     if (t.stride(-1) == 1 || cols == 1) {
@@ -181,7 +185,7 @@ Seed seed_of(const py::handle &v, const Tensor &x)
     if (!THPVariable_Check(v.ptr())) return { word(v, "seed"), {} };
     const Tensor t = py::cast<Tensor>(v);
     if (t.scalar_type() != at::kLong || t.numel() != 1 || t.device() != x.device()) refuse("a seed tensor is one int64 on the input's device");
-    return { 0, t };
+    return { 0, flat(t) };
 }
 
 void check_share(double p)
@@ -254,7 +258,7 @@ Normed run_norm(const Tensor &x, const Tensor &weight, const Tensor &bias, doubl
     if (residual.defined()) o.s = like(x);
     if (backward) o.stats = at::empty({ (int64_t)n, 2 }, x.options().dtype(at::kFloat).requires_grad(false));
     const Matrix m = matrix(x), r = matrix(residual);
-    const Tensor w = weight.defined() ? weight.contiguous() : weight, b = bias.defined() ? bias.contiguous() : bias;
+    const Tensor w = flat(weight), b = flat(bias);
     const vms_layernorm_args a = { sizeof a, type_of(x), n, cols, m.ptr(), r.ptr(), ptr(w), ptr(b), o.y.data_ptr(), ptr(o.s),
                                    (float *)ptr(o.stats), m.ld, r.ld, cols, cols, eps, mask };
     call(vms_layernorm, "vms_layernorm", a, x);
@@ -312,7 +316,7 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
             if (need_w) dweight = at::empty({ (int64_t)cols }, options);
             if (need_b) dbias = at::empty({ (int64_t)cols }, options);
             const Matrix m = matrix(dy), e = matrix(ds), k = matrix(s);
-            const Tensor w = weight.defined() ? weight.contiguous() : weight;
+            const Tensor w = flat(weight);
             vms_layernorm_backward_args a = { sizeof a, type_of(s), n, cols, m.ptr(), e.ptr(), k.ptr(), ptr(w), (const float *)ptr(saved[1]), dres.data_ptr(),
                                               ptr(dx), ptr(dweight), ptr(dbias), m.ld, e.ld, k.ld, cols, cols,
                                               mask, nullptr, 0 };
@@ -514,8 +518,8 @@ Tensor low_rank_add(const Tensor &y, const Tensor &x_, const Tensor &a_, const T
     const py::gil_scoped_release go;
     // What lies in the memory that the sum goes to is read from a copy: workgroups write columns of a row whose x others still read
     const auto apart = [&](const Tensor &t) { return inplace && shares(y, t) ? t.clone() : t; };
-    const Tensor x = apart(x_), a = apart(a_).contiguous(), b = apart(b_).contiguous();
-    const Batch batch = { factor, apart(scales), apart(starts), apart(which) };
+    const Tensor x = apart(x_), a = flat(apart(a_)), b = flat(apart(b_));
+    const Batch batch = { factor, flat(apart(scales)), flat(apart(starts)), flat(apart(which)) };
     if (wanted({ &y, &x, &a, &b })) return LowRankAdd::apply(y, x, a, b, batch, inplace);
     const Tensor out = run_low_rank(y, x, a, b, batch, inplace).first;
     if (inplace) y.unsafeGetTensorImpl()->bump_version();       // as a node's mark_dirty does: what was saved of y is noticed

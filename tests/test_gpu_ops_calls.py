@@ -177,3 +177,35 @@ def test_a_sum_in_place_that_autograd_forbids_changes_nothing():
     with torch.inference_mode():
         want = ops.low_rank_add(inner, x, a, b)
         assert ops.low_rank_add(inner, x, a, b, inplace=True) is inner and torch.equal(inner, want)
+
+
+def test_negative_views():
+    z = torch.randn(6, 40, 2, device="cuda")
+    x = torch._neg_view(z[..., 0].contiguous())
+    assert x.is_neg()
+    plain = x.resolve_neg()
+    w = torch._neg_view(torch.ones(40, device="cuda"))
+    a, b = torch._neg_view(torch.randn(4, 40, device="cuda")), torch._neg_view(torch.randn(40, 4, device="cuda"))
+    scale = torch._neg_view(torch.ones(1, device="cuda"))
+    some = [t.resolve_neg() for t in (w, a, b, scale)]
+    assert torch.equal(ops.dropout(x, 0.5, 1, residual=x), ops.dropout(plain, 0.5, 1, residual=plain))
+    assert torch.equal(ops.layer_norm(x, w, w), ops.layer_norm(plain, some[0], some[0]))
+    assert torch.equal(ops.low_rank_add(x, x, a, b, scale), ops.low_rank_add(plain, plain, *some[1:]))
+    with pytest.raises(ValueError):
+        ops.low_rank_add(x, x, a, b, inplace=True)
+    for make in (lambda v: ops.dropout(v, 0.5, 1), lambda v: ops.layer_norm(v, w), lambda v: ops.low_rank_add(v, v, a, b, scale)):
+        got = []
+        for v, dy in ((x, x), (plain, plain)):
+            leaf = v.detach().requires_grad_(True)
+            got.append(torch.autograd.grad(make(leaf), leaf, dy)[0])
+        assert torch.equal(got[0], got[1])
+
+
+def test_transforms_of_functions_are_refused():
+    """They hand wrappers to a function, which the operators do not see through"""
+    x, w = torch.randn(4, 6, 16, device="cuda"), torch.randn(16, device="cuda")
+    a, b = torch.randn(4, 16, device="cuda"), torch.randn(16, 4, device="cuda")
+    for f in (lambda v: ops.dropout(v, 0.5, 1), lambda v: ops.layer_norm(v, w), lambda v: ops.low_rank_add(v, v, a, b)):
+        for transformed in (lambda: torch.vmap(f)(x), lambda: torch.func.grad(lambda v: f(v).sum())(x[0]), lambda: torch.func.jvp(f, (x[0],), (x[0],))):
+            with pytest.raises((RuntimeError, ValueError)):
+                transformed()
