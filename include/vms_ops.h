@@ -118,8 +118,9 @@ int vms_layernorm_backward(const vms_layernorm_backward_args *a, void *stream);
  * d_y = d_out (same stride): the sum is made in place, and rows of no request are not touched.
  *
  * d_hidden (vms_lowrank_hidden_bytes, 16-byte aligned) receives scale * x a^T: workspace of the forward
- * pass, and what the backward pass reads, in a layout of the library's own with 16 bits or more of each
- * value (one that float16 does not hold is an infinity there, as in a program that stores it).    */
+ * pass, and what the backward pass reads, in a layout of the library's own.  In 16 bits a value is kept as
+ * two numbers of the type (what the first leaves in the second): to 2^-16 of it in bfloat16, to 2^-22 or
+ * 2^-25 in float16, where one beyond 65504 is an infinity, as in a program that stores it.             */
 #define VMS_LOWRANK_MAX_RANK 128
 typedef struct vms_lowrank_args {
     uint32_t struct_size;        /* sizeof(vms_lowrank_args)                                        */

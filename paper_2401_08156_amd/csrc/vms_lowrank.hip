@@ -181,11 +181,11 @@ DI bool find_tile(const Requests &q, u32 tile, Tile *out)
 
 // ---- down: hidden[row][j] = scale sum_k x[row][k] w[j][k] ------------------------------------------------------------
 
-// What a batch's hidden values are kept as.  They are sums, and the products that read them take the type of the tensors.  In
-// 16 bits a value of a small batch goes through as two, itself rounded and what that left, in two planes; that costs
-// nothing there.  In a large one it is rounded, half a step of the type for each term of a sum, as a program would that
-// stores x a^T: the second plane's reads from the caches take 106 us instead of 89 in `outer` and 105 instead of 93 in `up`
-// (8192 rows, 4096 -> 16384, rank 64).
+// What a batch's hidden values are kept as.  They are sums, and the products that read them take the type of the tensors: in
+// 16 bits a value goes through as two of the type, itself rounded and what that left, in two planes.  An output is
+// rounded once then, whatever the batch: the two hold a value to 2^-16 of it in bfloat16, to 2^-22 in float16 (to 2^-25 where
+// it is small; one beyond 65504 is an infinity).  A single rounded value would save `outer` 16 us of 93 (8192 rows, 4096 -> 16384,
+// rank 64) and `up` nothing, and make the outputs' error 1.4 times as large.
 // The values are laid out twice, in the order in which the lanes of `up` and of `outer` read them, padded to 16 rows.
 // Where there are not tiles enough for the compute units, workgroups share the summed dimension and leave parts of the sums,
 // in 32 bits: [splits][rows][padded].
@@ -193,7 +193,7 @@ struct Hidden {
     void *up;                   // [planes][rows / 16][padded / EPL][16][EPL]
     void *outer;                // 16 bits: [planes][rows / 8][padded][8]; 32 bits: [rows][padded]
     float *parts;               // not null: what `down` leaves
-    u32 splits, padded, planes;
+    u32 splits, padded;
     bool folded;                // the parts are put together in `up` and `outer` before they are read
 };
 
@@ -239,7 +239,6 @@ DI void store_hidden(const Hidden &h, const f32x4 &v, u64 row, u32 col, u32 spli
     }
 #pragma unroll
     for (int k = 0; k < Mma<T>::PLANES; k++) {
-        if (k && h.planes == 1) break;
         const u64 from = k * plane(rows, h.padded);
         *(typename Some<T, 4>::type *)((T *)h.up + from + up_place<T>(row, col, h.padded)) = o[k];
 #pragma unroll
@@ -550,7 +549,6 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
     const u32 last = rows ? rows - 1 : 0;
     const u64 row0 = t.row + (rows ? first : 0);    // rows beyond the tile are its last one again, and not stored
     Frag h[PLANES][MR][JS];
-    const bool two = PLANES == 2 && p.h.planes == 2;
 #pragma unroll
     for (int i = 0; i < MR; i++) {
         const u64 row = row0 + min(i * 16 + m, last);
@@ -564,7 +562,7 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
             } else if (!p.h.parts) {
 #pragma unroll
                 for (int k = 0; k < PLANES; k++)
-                    if (k == 0 || two) h[k][i][s] = *(const Frag *)((const T *)p.h.up + k * plane(p.q.rows, p.h.padded) + up_place<T>(row, j, p.h.padded));
+                    h[k][i][s] = *(const Frag *)((const T *)p.h.up + k * plane(p.q.rows, p.h.padded) + up_place<T>(row, j, p.h.padded));
             } else {
                 float v[EPL] = {};
                 const float *from = p.h.parts + row * p.h.padded + j;
@@ -655,11 +653,9 @@ __global__ __launch_bounds__(256) void lowrank_up_kernel(const UpParams p)
                 for (int s = 0; s < JS; s++) {
                     const Frag b = to[panel_place<CPR, SLAB / 4>(n, s * (STEP / EPL) + group)];
 #pragma unroll
-                    for (int i = 0; i < MR; i++) acc[i][q] = mma(b, h[0][i][s], acc[i][q]);
-                    if (two) {
+                    for (int k = 0; k < PLANES; k++)
 #pragma unroll
-                        for (int i = 0; i < MR; i++) acc[i][q] = mma(b, h[PLANES - 1][i][s], acc[i][q]);
-                    }
+                        for (int i = 0; i < MR; i++) acc[i][q] = mma(b, h[k][i][s], acc[i][q]);
                 }
             }
 #pragma unroll
@@ -774,7 +770,8 @@ __global__ __launch_bounds__(256) void lowrank_up_few_kernel(const UpParams p)
                 for (int e = 0; e < EPL; e++) h[r][e] += from[e];
             }
         } else {
-            for (u32 k = 0; k < p.h.planes; k++) {
+#pragma unroll
+            for (int k = 0; k < Mma<T>::PLANES; k++) {
                 const Frag f = *(const Frag *)((const T *)p.h.up + k * plane(p.q.rows, p.h.padded) + up_place<T>(row, chunk * EPL, p.h.padded));
 #pragma unroll
                 for (int e = 0; e < EPL; e++) h[r][e] += (float)f[e];
@@ -899,7 +896,6 @@ __global__ __launch_bounds__(64) void lowrank_fold_kernel(const FoldParams p)
         }
 #pragma unroll
         for (int k = 0; k < Mma<T>::PLANES; k++) {
-            if (k && h.planes == 1) break;
             const u64 from = k * plane(p.rows, h.padded);
             if (up) *(Four *)((T *)h.up + from + up_place<T>(row + r, col, h.padded)) = o[k];
             if (outer) *(Four *)((T *)h.outer + from + (sizeof(T) == 4 ? outer_place<T>(row + r, col, h.padded) : outer_place<T>(row, col + r, h.padded))) = c[k];
@@ -918,7 +914,6 @@ struct OuterJob {
 struct OuterParams {
     OuterJob job[2];
     Requests q;
-    u32 planes;
 };
 
 // two 16-bit elements of each of two registers, swapped: (a0 b0) and (a1 b1) of (a0 a1), (b0 b1)
@@ -928,7 +923,7 @@ DI u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302
 // Rows t to t + 31 of CQ columns a lane, and what belongs to them of hidden; 0 in the place of rows that are not from lo to
 // hi - 1, whatever lies there.  t is a multiple of 8.  WHOLE: all of these rows, and whole panels.
 template <class T, int CQ, int NR, bool WHOLE>
-DI void outer_load(const OuterJob &o, u32 t, u32 lo, u32 hi, u32 rows, u32 col, int cols, u32 (&v)[8][CQ / 2], typename Mma<T>::Frag (&h)[2][NR], bool two)
+DI void outer_load(const OuterJob &o, u32 t, u32 lo, u32 hi, u32 rows, u32 col, int cols, u32 (&v)[8][CQ / 2], typename Mma<T>::Frag (&h)[2][NR])
 {
     typedef typename Mma<T>::Frag Frag;
     const u32 lane = lane_id(), m = lane & 15, r0 = t + (lane >> 4) * 8;
@@ -944,7 +939,6 @@ DI void outer_load(const OuterJob &o, u32 t, u32 lo, u32 hi, u32 rows, u32 col, 
     }
 #pragma unroll
     for (int k = 0; k < 2; k++) {
-        if (k && !two) break;
 #pragma unroll
         for (int j = 0; j < NR; j++) {
             h[k][j] = Frag{};
@@ -961,7 +955,7 @@ DI void outer_load(const OuterJob &o, u32 t, u32 lo, u32 hi, u32 rows, u32 col, 
 
 // acc[q][j] += v^T hidden for column q of a lane and the j-th 16 of the rank
 template <class T, int CQ, int NR>
-DI void outer_add(const u32 (&v)[8][CQ / 2], const typename Mma<T>::Frag (&h)[2][NR], bool two, f32x4 (&acc)[CQ][NR])
+DI void outer_add(const u32 (&v)[8][CQ / 2], const typename Mma<T>::Frag (&h)[2][NR], f32x4 (&acc)[CQ][NR])
 {
     typedef typename Mma<T>::Frag Frag;
 #pragma unroll
@@ -976,17 +970,12 @@ DI void outer_add(const u32 (&v)[8][CQ / 2], const typename Mma<T>::Frag (&h)[2]
         __builtin_memcpy(&a, low, sizeof a);
         __builtin_memcpy(&b, high, sizeof b);
 #pragma unroll
-        for (int j = 0; j < NR; j++) {
-            acc[q][j] = mma(a, h[0][j], acc[q][j]);
-            acc[q + 1][j] = mma(b, h[0][j], acc[q + 1][j]);
-        }
-        if (two) {
+        for (int k = 0; k < 2; k++)
 #pragma unroll
             for (int j = 0; j < NR; j++) {
-                acc[q][j] = mma(a, h[1][j], acc[q][j]);
-                acc[q + 1][j] = mma(b, h[1][j], acc[q + 1][j]);
+                acc[q][j] = mma(a, h[k][j], acc[q][j]);
+                acc[q + 1][j] = mma(b, h[k][j], acc[q + 1][j]);
             }
-        }
     }
 }
 
@@ -1071,10 +1060,10 @@ __global__ __launch_bounds__(256) void lowrank_outer_kernel(const OuterParams p)
                     u32 v[8][CQ / 2];
                     typename Mma<T>::Frag h[2][NR];
                     if (LIKELY(whole))
-                        outer_load<T, CQ, NR, true>(o, t, begin, end, p.q.rows, col, cols, v, h, p.planes == 2);
+                        outer_load<T, CQ, NR, true>(o, t, begin, end, p.q.rows, col, cols, v, h);
                     else
-                        outer_load<T, CQ, NR, false>(o, t, begin, end, p.q.rows, col, cols, v, h, p.planes == 2);
-                    outer_add<T, CQ, NR>(v, h, p.planes == 2, acc);
+                        outer_load<T, CQ, NR, false>(o, t, begin, end, p.q.rows, col, cols, v, h);
+                    outer_add<T, CQ, NR>(v, h, acc);
                 }
             }
         }
@@ -1266,10 +1255,8 @@ Cut forward_cut(const vms_lowrank_args *a)
     return c;
 }
 
-u32 planes_of(const vms_lowrank_args *a) { return a->dtype != VMS_F32 && a->rows * a->rank <= 1 << 16 ? 2 : 1; }
-
 // bytes of one layout with its planes
-size_t laid_out(const vms_lowrank_args *a) { return (a->rows + 15) / 16 * 16 * padded_rank(a->rank) * type_bytes(a->dtype) * planes_of(a); }
+size_t laid_out(const vms_lowrank_args *a) { return (a->rows + 15) / 16 * 16 * padded_rank(a->rank) * (a->dtype == VMS_F32 ? 4 : 2 * 2); }
 
 size_t parts_bytes(const vms_lowrank_args *a, const Cut &c) { return c.splits > 1 ? (size_t)c.splits * a->rows * padded_rank(a->rank) * 4 : 0; }
 
@@ -1277,11 +1264,11 @@ size_t hidden_bytes(const vms_lowrank_args *a, const Cut &c) { return (c.splits 
 
 Hidden hidden_at(const vms_lowrank_args *a, const Cut &c, void *at)
 {
-    const u32 padded = padded_rank(a->rank), planes = planes_of(a);
+    const u32 padded = padded_rank(a->rank);
     char *const p = (char *)at;
-    if (c.splits == 1) return Hidden{ p, p + laid_out(a), nullptr, 1, padded, planes, false };
-    if (c.folded) return Hidden{ p, p + laid_out(a), (float *)(p + 2 * laid_out(a)), c.splits, padded, planes, true };
-    return Hidden{ nullptr, nullptr, (float *)p, c.splits, padded, planes, false };
+    if (c.splits == 1) return Hidden{ p, p + laid_out(a), nullptr, 1, padded, false };
+    if (c.folded) return Hidden{ p, p + laid_out(a), (float *)(p + 2 * laid_out(a)), c.splits, padded, true };
+    return Hidden{ nullptr, nullptr, (float *)p, c.splits, padded, false };
 }
 
 int check(const vms_lowrank_args *a)
@@ -1532,7 +1519,7 @@ int backward(const vms_lowrank_backward_args *a, void *stream)
         rc = fold<T>(some, stream);
         if (rc) return rc;
     }
-    OuterParams o = { { l.db, l.da }, requests_of(&f), h.planes };
+    OuterParams o = { { l.db, l.da }, requests_of(&f) };
     o.job[0].v = a->d_dout;
     o.job[0].ldv = a->lddout;
     o.job[0].hidden = h.outer;

@@ -49,3 +49,55 @@ def test_sums_larger_than_the_last_cache(rank, length, dtype):
         before = out.detach().clone()
         y2 = ops.low_rank_add(y, x, a if adapters > 1 else a[0], b if adapters > 1 else b[0], **args, inplace=True)
         assert y2 is y and torch.equal(y, before)
+
+
+def one_of_each_column(rows, cols, dtype, seed):
+    """a matrix with one number in each column, in a row of its own choice; (on the GPU, in 64 bits)"""
+    g = torch.Generator().manual_seed(seed)
+    v = torch.zeros(rows, cols, dtype=torch.float64)
+    v[torch.randint(0, rows, (cols,), generator=g), torch.arange(cols)] = torch.randn(cols, generator=g, dtype=torch.float64)
+    v = v.to(dtype)
+    return v.cuda(), v.double()
+
+
+def product(dtype, n, h, e_h, v):
+    """How far h v may be off, rounded to the type, where every element of it is one product (of n that are summed): h by e_h and
+    by what two values of the type leave of it (u of the first, u of that by the second), the product by its roundings in 32 bits"""
+    u, chain = oo.unit(dtype), (n / 4 + oo.DEPTH) * oo.EMMA
+    e = e_h + (0.0 if dtype == torch.float32 else u * u * (h.abs() + e_h) + oo.tiny(dtype))
+    want, off = h @ v, e @ v.abs() + chain * ((h.abs() + e) @ v.abs())
+    return want, u * want.abs() + (1 + u) * off + oo.tiny(dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,rank,tokens", [(3, 16, False), (37, 8, False), (700, 128, False), (1100, 64, False), (2300, 32, False), (5000, 16, False), (2100, 64, False),
+                                              (40, 16, True), (300, 64, True), (600, 128, True)])
+def test_hidden_values_are_not_rounded_to_the_type(rows, rank, tokens, dtype):
+    """x a^T and dout b are sums in 32 bits; the products that read them round once, to their outputs, in batches of every size.
+    With one number in each column of b, dout, a or x every output is one product, so that a rounding in between would show."""
+    k, n, scale = (4200 if rows == 2100 else 96), 160, 0.5
+    normal = lambda *s, seed: (lambda t: (t.cuda(), t.double()))(torch.randn(s, generator=torch.Generator().manual_seed(seed), dtype=torch.float64).to(dtype))
+    starts = torch.arange(rows + 1, dtype=torch.int32, device="cuda") if tokens else None
+    which = torch.zeros(rows, dtype=torch.int32, device="cuda") if tokens else None
+
+    def run(x, a, b, dout):
+        leaves = [t[None] if i and tokens else t for i, t in enumerate((x, a, b))]
+        for t in leaves:
+            t.requires_grad_(True)
+        out = ops.low_rank_add(torch.zeros(rows, b.shape[0], dtype=dtype, device="cuda"), *leaves, scale=scale, starts=starts, which=which)
+        return out, [g.reshape(t.shape) for g, t in zip(torch.autograd.grad(out, leaves, dout), (x, a, b))]
+    hidden = lambda v, w: (scale * (v @ w.t()), ((v.shape[1] / 4 + oo.DEPTH) * oo.EMMA + 2 * oo.E32) * abs(scale) * (v.abs() @ w.abs().t()))
+    # hidden = scale x a^T through b and dout
+    (x, x64), (a, a64) = normal(rows, k, seed=1), normal(rank, k, seed=2)
+    (bt, bt64), (dout, dout64) = one_of_each_column(rank, n, dtype, 3), one_of_each_column(rows, n, dtype, 4)
+    h, e_h = hidden(x64, a64)
+    out, (_, _, db) = run(x, a, bt.t().contiguous(), dout)
+    oo.assert_within("out", out, *product(dtype, rank, h, e_h, bt64))
+    oo.assert_within("db", db.t(), *product(dtype, rows, h.t(), e_h.t(), dout64))
+    # dhidden = scale dout b through a and x
+    (dout, dout64), (b, b64) = normal(rows, n, seed=5), normal(n, rank, seed=6)
+    (a, a64), (x, x64) = one_of_each_column(rank, k, dtype, 7), one_of_each_column(rows, k, dtype, 8)
+    h, e_h = hidden(dout64, b64.t())
+    _, (dx, da, _) = run(x, a, b, dout)
+    oo.assert_within("dx", dx, *product(dtype, rank, h, e_h, a64))
+    oo.assert_within("da", da, *product(dtype, rows, h.t(), e_h.t(), x64))
