@@ -156,8 +156,9 @@ DI u32 die_order(u32 b, u32 n)
 const u32 OPS_CUS = 256;        // compute units of the device that the grids are sized for
 
 // Does a call that reads and writes so many bytes leave nothing of them in the last cache (256 MiB)?  Then its accesses are
-// marked as not to be kept: dropout of 4096 x 16384 in 16 bits, 268 MB, takes 48 us, 51 without the marks.  A smaller call's
-// output may be found there by the next kernel.
+// marked as not to be kept: dropout of 8192 x 16384 in 16 bits, 537 MB, takes 90 us, 97 without the marks.  What just fills the
+// cache is better left in it (4096 x 16384: 42 us, 45 with them), and a smaller call's output may be found there by the next
+// kernel.
 inline bool passes_by(u64 bytes) { return bytes > 256u << 20; }
 
 template <class P>
