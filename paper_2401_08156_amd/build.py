@@ -35,16 +35,26 @@ OPS_FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-shared", "-fPIC", "
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 
+def _torch():
+    """PyTorch, or None where it is not installed: the library does not need it, the autograd nodes do."""
+    try:
+        import torch
+    except ImportError:
+        return None
+    return torch
+
+
 def _stale():
-    if not os.path.exists(LIB) or not os.path.exists(EXT):
+    built = [LIB] if _torch() is None else [LIB, EXT]
+    if not all(os.path.exists(f) for f in built):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(EXT))
+    t = min(os.path.getmtime(f) for f in built)
     deps = [os.path.join(CSRC, s) for s in SOURCES + OPS_SOURCES + [EXT_SOURCE] + HEADERS]
     return any(os.path.exists(d) and os.path.getmtime(d) > t for d in deps)
 
 
 def build(force=False, save_temps_dir=None):
-    """Build libvmsreplay.so and _vms_torch.so next to this file; returns the library's path."""
+    """Build libvmsreplay.so and, where PyTorch is installed, _vms_torch.so next to this file; returns the library's path."""
     if not force and not _stale():
         return LIB
     jobs = [(s, flags) for group, flags in ((SOURCES, HIPCC_FLAGS), (OPS_SOURCES, OPS_FLAGS)) for s in group]
@@ -56,15 +66,19 @@ def build(force=False, save_temps_dir=None):
             obj = os.path.join(objects, source + ".o")
             cmd = ["hipcc"] + [f for f in flags if f != "-shared"] + ["-c", os.path.join(CSRC, source), "-o", obj]
             return obj, _run(cmd + ["--save-temps"] * bool(save_temps_dir), save_temps_dir or CSRC)
-        ext = os.path.join(objects, EXT_SOURCE + ".o")
+        ext, out = os.path.join(objects, EXT_SOURCE + ".o"), []
         with ThreadPoolExecutor(4) as pool:
-            node = pool.submit(_run, _ext_command() + ["-c", os.path.join(CSRC, EXT_SOURCE), "-o", ext], CSRC)
-            done = list(pool.map(compile_one, jobs)) + [(None, node.result())]
-        out = "\n".join(text for _, text in done if text.strip())
-        done.pop()
-        _run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + [obj for obj, _ in done], CSRC)
-        _run(["g++", "-shared", "-o", EXT, ext, "-L" + _torch_dir("lib"), "-L" + _HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN"]
-             + ["-l" + l for l in ("c10", "c10_hip", "torch", "torch_cpu", "torch_python")], CSRC)
+            node = _torch() and pool.submit(_run, _ext_command() + ["-c", os.path.join(CSRC, EXT_SOURCE), "-o", ext], CSRC)
+            done = list(pool.map(compile_one, jobs))
+            out += [text for _, text in done]
+            out.append(_run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + [obj for obj, _ in done], CSRC))
+            if node:
+                out.append(node.result())
+                out.append(_run(["g++", "-shared", "-o", EXT, ext, "-L" + _torch_dir("lib"), "-L" + _HERE, "-l:" + os.path.basename(LIB),
+                                 "-Wl,-rpath,$ORIGIN"] + ["-l" + l for l in ("c10", "c10_hip", "torch", "torch_cpu", "torch_python")], CSRC))
+            else:
+                out.append("no PyTorch: " + os.path.basename(EXT) + " (the operators for its tensors) is not built")
+    out = "\n".join(text for text in out if text.strip())
     if out:
         print(out)
     return LIB
@@ -89,5 +103,5 @@ def _run(cmd, cwd):
     r = subprocess.run(cmd, cwd=cwd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     out = "\n".join(l for l in r.stdout.splitlines() if "packed-fp32-ops" not in l)
     if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + out)
+        raise RuntimeError(cmd[0] + " failed:\n" + out)
     return out
