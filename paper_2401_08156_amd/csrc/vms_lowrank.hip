@@ -1182,7 +1182,7 @@ const u32 DOWN_WAVES = 8;       // of a workgroup; twice that where the rank lea
 // are not there; at most four, two or one as the rank leaves registers; and half as many as long as there are then still no more
 // tiles than compute units: larger tiles read the weights less often, but compute units without a tile read nothing, and a few
 // tiles more than one for each take as long as two (24 requests of 6007 rows in all, 4096 -> 4096: rank 64 46 us forward with
-// tiles of 32 rows, 53 with 16; rank 32 41 and 44).
+// tiles of 32 rows, 54 with 16; rank 32 40 and 42).
 u32 tile_of(const vms_lowrank_args *a)
 {
     const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
@@ -1203,7 +1203,7 @@ Cut cut_of(const vms_lowrank_args *a, u64 in)
     const u64 requests = a->d_starts ? a->n_requests : 1, each = requests ? a->rows / requests : a->rows;
     // Shared weights save reads from the caches, as many as there are steps and ranks, and cost a launch: 8192 rows at rank 64
     // take 71 us with them and 82 without over 16384 columns, 26 and 23 over 4096; at rank 128 and 4096 columns the whole
-    // step of 8192 rows 238 and 252 us.
+    // step of 8192 rows 225 and 230 us.
     const bool shared = a->rank > 32 && in * padded_rank(a->rank) >= 1u << 19 && each >= 128 && a->rows >= 2048;
     c.tile16 = shared ? 8 : tile_of(a);
     const u64 tiles = tiles_of(a, c.tile16), slabs = in * type_bytes(a->dtype) / SLAB_BYTES;
@@ -1300,7 +1300,7 @@ UpCut up_cut(const vms_lowrank_args *a, u64 cols, bool base)
     c.tiles = (u32)tiles;
     const u64 trip = few ? 256 : (c.tile16 == 1 ? 4 : 1) * (SLAB_BYTES / type_bytes(a->dtype)), all = (cols + trip - 1) / trip;
     // Workgroups enough for four on every compute unit before one takes a second trip; no more than that where each has to
-    // find its request first (24 requests, 6007 rows, 4096 -> 4096, rank 32: 22 us, 25 with as many again; one token each of
+    // find its request first (24 requests, 6007 rows, 4096 -> 4096, rank 64: 46 us forward, 49 with as many again; one token each of
     // 96 requests, 4096 -> 16384, rank 16: 12 us, 16 with three times as many).
     u64 trips = (all * tiles + (a->d_starts || few ? OPS_CUS * 4 - 1 : 0)) / (OPS_CUS * 4);
     trips = trips < 1 ? 1 : trips > 8 ? 8 : trips;

@@ -141,7 +141,7 @@ __global__ __launch_bounds__(SINGLE ? 256 : 1024) void norm_kernel(const NormPar
     typedef typename Eight<T>::type Raw;
     for (u32 row = SINGLE ? blockIdx.x * 4 + wave : blockIdx.x; row < p.rows; row += step) {
         // What the row needs is on its way before the first of it is waited for, the weights too where registers hold them
-        // (4099 x 5120 in 16 bits: 28 us, 32 with each load waited for before the next).
+        // (4099 x 5120 in 16 bits: 25 us, 28 with each load waited for before the next).
         const bool AHEAD = NG < 4, WEIGHTS_AHEAD = AHEAD && NG * sizeof(T) <= 8;
         Raw x[NG], r[NG], w[NG], b[NG];
         const auto fetch = [&](int g) {
