@@ -146,7 +146,7 @@ variable_list first_order(variable_list grads, const variable_list &from, std::i
         for (uint32_t k = 0; k < here->num_outputs(); k++)
             if ((by.begin()[i] >> k & 1) && here->next_edge(k).is_valid()) edges.push_back(here->next_edge(k));
         if (edges.empty()) continue;
-        const auto node = std::make_shared<FirstOrder>();
+        const std::shared_ptr<FirstOrder> node(new FirstOrder, torch::autograd::deleteNode);       // (long graphs are taken down without recursion)
         node->set_next_edges(std::move(edges));
         grads[i] = grads[i].detach();
         torch::autograd::set_history(grads[i], node);

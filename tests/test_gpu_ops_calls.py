@@ -209,3 +209,14 @@ def test_transforms_of_functions_are_refused():
         for transformed in (lambda: torch.vmap(f)(x), lambda: torch.func.grad(lambda v: f(v).sum())(x[0]), lambda: torch.func.jvp(f, (x[0],), (x[0],))):
             with pytest.raises((RuntimeError, ValueError)):
                 transformed()
+
+
+def test_a_long_graph_of_gradients_is_taken_down():
+    """A graph as deep as 30,000 operators, with a node that refuses behind each of them"""
+    x = torch.randn(2, 8, device="cuda", requires_grad=True)
+    y = x
+    for i in range(30000):
+        y = ops.dropout(y, 0.0, i)
+    g, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+    assert torch.equal(g.detach(), 2 * x.detach()) and g.requires_grad
+    del g, y
